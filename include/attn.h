@@ -260,6 +260,85 @@ int attn_bwd_strided(int dtype, const void* q, const attn_strides_t* sq, const v
                      int B, int H, int Hkv, int Nq, int Nk, int d_qk, int d_v, float scale, int causal,
                      void* workspace, size_t workspace_bytes, void* stream);
 
+/* Rotary positions of queries and keys, with the norms of their heads in the same pass (the paper starts from the Q and K that
+ * result).  For every row x of d numbers (a token of a head of q or of k):
+ *     n   = x * w / sqrt(mean(x^2) + eps)       with norm != 0 (w: q_weight or k_weight [d], element type; null: ones), else n = x
+ *     y_i = A (cos(a) n_i - sin(a) n_j),  y_j = A (sin(a) n_i + cos(a) n_j)        for the pairs (i, j) of the rotated dims
+ *     y_c = n_c                                                                    for the others
+ * The rotated dims are offset ... offset + rot - 1 of the head (rot and offset multiples of 16 and 8); pair p = 0 ... rot/2 - 1 is
+ * dims (offset + p, offset + rot/2 + p), or, with interleaved != 0, (offset + 2p, offset + 2p + 1); a = position * freqs[p], as if
+ * exact: far positions lose nothing; A = amplitude.  Contexts longer than trained ones are a matter of freqs and amplitude.
+ * positions: int32, one per token, any value, token n of sequence b at positions[b * positions_batch + n] (positions_batch = 0: the
+ * same for every sequence); null: n.  Sums and products are in fp32; the result is rounded once, to the element type.
+ *   tensors: views as in attn_fwd_strided, q and q_out [B, N, H, d], k and k_out [B, N, Hkv, d] (B = 1 for packed tokens), d 64,
+ *   96, 128, 192 or 256; k and k_out may both be null.  An output may be its input (same address and strides); any other overlap
+ *   is an error of the caller's. */
+typedef struct attn_rope {
+    const float* freqs;         /* [rot / 2], fp32, device */
+    const int* positions;       /* device, or null */
+    long long positions_batch;
+    int rot, offset, interleaved;
+    float amplitude;
+    int norm;
+    float eps;                  /* >= 0 */
+    const void *q_weight, *k_weight;
+} attn_rope_t;
+int attn_rope_fwd(int dtype, const attn_rope_t* rope, const void* q, const attn_strides_t* sq, const void* k, const attn_strides_t* sk,
+                  void* q_out, const attn_strides_t* sqo, void* k_out, const attn_strides_t* sko,
+                  int B, int N, int H, int Hkv, int d, void* stream);
+/* Its backward pass: dq and dk are the gradients of q_out and k_out, dq_in and dk_in receive those of q and k (an output may be
+ * one of the pass's inputs of the same tensor), dq_weight and dk_weight (fp32 [d], each may be null) those of the weights, summed
+ * over all rows in fp32 in an order that depends on the sizes alone.  q and k are the forward pass's inputs, needed with norm != 0
+ * only (else they and their strides may be null).  workspace: attn_rope_workspace_bytes(...) bytes, 256-byte aligned, for the sums;
+ * may be null where both dq_weight and dk_weight are.  Two kernels with the sums, one without. */
+size_t attn_rope_workspace_bytes(int B, int N, int H, int Hkv, int d);
+int attn_rope_bwd(int dtype, const attn_rope_t* rope, const void* dq, const attn_strides_t* sdq, const void* dk, const attn_strides_t* sdk,
+                  const void* q, const attn_strides_t* sq, const void* k, const attn_strides_t* sk,
+                  void* dq_in, const attn_strides_t* sdqi, void* dk_in, const attn_strides_t* sdki, float* dq_weight, float* dk_weight,
+                  int B, int N, int H, int Hkv, int d, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A cache of keys and values in 4 or 8 bits, in pages: rows are quantised as they are written, read back, or attended to.
+ *   k, v           : codes, [pages, Hkv, page, d_qk * bits / 8] and [pages, Hkv, page, d_v * bits / 8] bytes, 16-byte aligned
+ *   k_scale, v_scale : [pages, Hkv, page, d_qk / 32] and [pages, Hkv, page, d_v / 32] bytes
+ * all contiguous, in device memory.  A row (token, KV head) is in blocks of 32 channels with one scale byte s each, which stands
+ * for 2^(s - 127) (255: the block is NaN); bits = 4: e2m1 codes (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), the
+ * even channel in the low half of the byte; bits = 8: e4m3 codes (largest value 448, 0x7f NaN).  (The block formats of the OCP
+ * Microscaling specification v1.0, which gfx950 converts in hardware.)  The scale is the least power of two with which no element
+ * of the block is cut off when it is rounded to nearest (ties to even); a block that holds an infinity or a NaN is NaN.  Rounding
+ * is exact arithmetic: codes and scales depend on the row's values alone.
+ *   page: tokens per page, a power of two, 16 ... 65536; pages * page <= 2^31 - 1; head dims as elsewhere.
+ * Slot s is token s % page of page s / page. */
+typedef struct attn_cache {
+    void *k, *k_scale, *v, *v_scale;
+    int pages, page, Hkv, d_qk, d_v, bits;
+} attn_cache_t;
+/* Quantises k [T, Hkv, d_qk] and v [T, Hkv, d_v] (token and head strides; `batch` is not used) into the slots slots[0 ... T-1] (int32,
+ * device).  A row whose slot is negative or past the cache is skipped (padding); the others must differ, or the bytes of a slot that is
+ * given twice are unspecified.  No other byte of the cache is touched. */
+int attn_cache_write(int dtype, const attn_cache_t* cache, const void* k, const attn_strides_t* sk, const void* v, const attn_strides_t* sv,
+                     const int* slots, int T, void* stream);
+/* The rows of these slots (any order, any number of times) as numbers of the element type: k [T, Hkv, d_qk], v [T, Hkv, d_v], contiguous;
+ * zeros where a slot is negative or past the cache.  bf16 holds every value that was written from 16-bit numbers; fp16 rounds and
+ * is infinite beyond its range. */
+int attn_cache_read(int dtype, const attn_cache_t* cache, const int* slots, int T, void* k, void* v, void* stream);
+/* Attention of Nq queries per sequence over that cache: sequence b has lens[b] keys (int32, device), key j in page
+ * block_table[b * table_width + j / page] (int32, device) at j % page.  q and o are views [B, Nq, H, d] as in attn_fwd_strided, lse [B, H, Nq]
+ * contiguous.  causal != 0: the last query is aligned with the last key (key j visible to query i iff j <= i + lens[b] - Nq).
+ *   - A query without a visible key (an empty batch slot, lens[b] = 0, or causal with fewer keys than queries) has o = 0 and
+ *     lse = -inf.  A negative length counts as 0, one beyond table_width * page as that.
+ *   - Entries of the table behind a sequence's last key are not read.  A page number outside the cache makes the rows that see
+ *     its keys NaN; nothing outside the tensors is touched.
+ *   - A key or value that is NaN reaches the queries that see it and no others; what the slots behind the last key hold (never
+ *     written, another sequence's, NaN) reaches none.
+ *   - Lengths and pages are read on the device: a captured call may be replayed with others.  Any Nq works; it is meant for few
+ *     (one token, a few drafted ones): a long chunk reads its keys back (attn_cache_read) for attn_varlen_fwd.
+ *   workspace: attn_cache_workspace_bytes(...) bytes, 256-byte aligned, contents ignored.  One kernel, and a merge where the table
+ *   is wide enough for a sequence to be divided. */
+size_t attn_cache_workspace_bytes(const attn_cache_t* cache, int B, int Nq, int H, int table_width);
+int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, void* o, const attn_strides_t* so, float* lse,
+                   const int* block_table, int table_width, const int* lens, int B, int Nq, int H, float scale, int causal,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
 /* Software 2^x of paper Sec. 3.1.3 (range reduction + degree-n minimax polynomial, p0 = 1, Horner
  * with FMAs, exponent splice), provided to measure its accuracy on this hardware; attn_fwd does not
  * use it (v_exp_f32 and the FMAs share one issue port on CDNA4, so emulation cannot add throughput:

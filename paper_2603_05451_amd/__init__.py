@@ -8,8 +8,10 @@ from __future__ import annotations
 
 import array
 import ctypes
+import math
 import os
 from functools import lru_cache
+from typing import NamedTuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libattn.so")
@@ -82,6 +84,21 @@ def lib():
         L.attn_varlen_fwd.restype = i
         L.attn_varlen_bwd.argtypes = [vp] * 11 + [i] * 7 + [f, i, vp, sz, vp]
         L.attn_varlen_bwd.restype = i
+        rp, cp = ctypes.POINTER(AttnRope), ctypes.POINTER(AttnCacheLayout)
+        L.attn_rope_fwd.argtypes = [i, rp] + [vp, sp] * 4 + [i] * 5 + [vp]
+        L.attn_rope_fwd.restype = i
+        L.attn_rope_workspace_bytes.argtypes = [i] * 5
+        L.attn_rope_workspace_bytes.restype = sz
+        L.attn_rope_bwd.argtypes = [i, rp] + [vp, sp] * 6 + [vp, vp] + [i] * 5 + [vp, sz, vp]
+        L.attn_rope_bwd.restype = i
+        L.attn_cache_write.argtypes = [i, cp, vp, sp, vp, sp, vp, i, vp]
+        L.attn_cache_write.restype = i
+        L.attn_cache_read.argtypes = [i, cp, vp, i, vp, vp, vp]
+        L.attn_cache_read.restype = i
+        L.attn_cache_workspace_bytes.argtypes = [cp, i, i, i, i]
+        L.attn_cache_workspace_bytes.restype = sz
+        L.attn_cache_fwd.argtypes = [i, cp, vp, sp, vp, sp, vp, vp, i, vp, i, i, i, f, i, vp, sz, vp]
+        L.attn_cache_fwd.restype = i
         L.attn_exp2_emulated.argtypes = [vp, vp, sz, i, vp]
         L.attn_exp2_emulated.restype = i
         L.attn_strerror.argtypes = [i]
@@ -435,3 +452,262 @@ def attn_bwd_noalloc(q, k, v, o, do, lse, scale, causal, dq, dk, dv, stream=None
                                   _dev(dk, "dk", k.shape, dt), _dev(dv, "dv", v.shape, dt), B, H, Hkv, N, dqk, dvd,
                                   float(scale), int(bool(causal)), _stream(stream)))
     return dq, dk, dv
+
+
+# ---- rotary positions and head norms; the quantised cache
+
+class AttnRope(ctypes.Structure):
+    """attn_rope_t of include/attn.h."""
+    _fields_ = [("freqs", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_batch", ctypes.c_longlong),
+                ("rot", ctypes.c_int), ("offset", ctypes.c_int), ("interleaved", ctypes.c_int), ("amplitude", ctypes.c_float),
+                ("norm", ctypes.c_int), ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
+
+
+class AttnCacheLayout(ctypes.Structure):
+    """attn_cache_t of include/attn.h."""
+    _fields_ = [("k", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("pages", ctypes.c_int), ("page", ctypes.c_int), ("Hkv", ctypes.c_int), ("d_qk", ctypes.c_int), ("d_v", ctypes.c_int),
+                ("bits", ctypes.c_int)]
+
+
+def _here(t, name, dtype, stream):
+    """Refuses a tensor of another type or device than the call's kernels run with."""
+    import torch
+    if not (t.is_cuda and t.dtype == dtype):
+        raise ValueError(f"{name} must be a {dtype} CUDA tensor")
+    device = stream.device.index if stream is not None else torch.cuda.current_device()
+    if t.device.index != device:
+        raise ValueError(f"{name} is on {t.device}, the call runs on device {device}: make its device the current one")
+
+
+def _rows(t, name, dtype, stream, shape=None):
+    """A [B, N, heads, d] or packed [T, heads, d] view as a 4-d one."""
+    _here(t, name, dtype, stream)
+    if t.dim() not in (3, 4) or (t.stride(-1) != 1 and t.shape[-1] != 1):
+        raise ValueError(f"{name} must be a [B, N, heads, d] or [T, heads, d] tensor with a contiguous last axis")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return t if t.dim() == 4 else t.unsqueeze(0)
+
+
+def _strides(t):
+    return None if t is None else ctypes.byref(AttnStrides(t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0,
+                                                           t.stride(2) if t.shape[2] > 1 else 0))
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rope(x, y, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, stream):
+    """attn_rope_t for rows x (4-d, of q) and y (of k, or None)."""
+    import torch
+    dt, (B, N, _, d) = x.dtype, x.shape
+    _here(freqs, "freqs", torch.float32, stream)
+    if freqs.dim() != 1 or not freqs.is_contiguous():
+        raise ValueError("freqs must be a contiguous fp32 CUDA tensor [rot / 2]")
+    batch = 0
+    if positions is not None:
+        _here(positions, "positions", torch.int32, stream)
+        if not positions.is_contiguous() or positions.shape not in ((N,), (B, N)):
+            raise ValueError(f"positions must be a contiguous int32 CUDA tensor [{N}] or [{B}, {N}]")
+        batch = N if positions.dim() == 2 else 0
+    if eps is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("weights without eps: eps asks for the norms")
+    for w, name, there in ((q_weight, "q_weight", True), (k_weight, "k_weight", y is not None)):
+        if w is not None:
+            _here(w, name, dt, stream)
+            if not there or w.shape != (d,) or not w.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {dt} CUDA tensor [{d}]" + ("" if there else ", and there is no k"))
+    return AttnRope(freqs.data_ptr(), _address(positions), batch, 2 * freqs.shape[0], int(offset), int(bool(interleaved)), float(amplitude),
+                    int(eps is not None), 0.0 if eps is None else float(eps), _address(q_weight), _address(k_weight))
+
+
+def attn_rope_freqs(rot, base=10000.0, factor=1.0, original=None, low=1.0, high=32.0, device="cuda"):
+    """The rot / 2 frequencies (radians per position, fp32) of rotary positions: base^(-2i / rot).  For contexts `factor` times longer
+    than the trained ones: without `original` every frequency is divided by factor (positions are interpolated); with the trained
+    length in `original` by parts (Peng et al. 2023, "YaRN", Sec. 3.2): frequencies that turn more than `high` times within it stay, those
+    that turn less than `low` times are divided, linearly in the number of turns between."""
+    import torch
+    if rot <= 0 or rot % 2 or not (base > 0 and factor > 0):
+        raise ValueError("rot must be even and positive, base and factor positive")
+    f = float(base) ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    if original is None:
+        f = f / factor
+    else:
+        if not (original > 0 and high > low):
+            raise ValueError("original must be positive and high above low")
+        stay = ((original * f / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+        f = f * (stay + (1 - stay) / factor)
+    return f.float().to(device)
+
+
+def attn_rope_fwd(q, k, freqs, positions=None, interleaved=False, offset=0, amplitude=1.0, eps=None, q_weight=None, k_weight=None,
+                  q_out=None, k_out=None, stream=None):
+    """Rotary positions of q [B,N,H,d] and k [B,N,Hkv,d] (or packed [T,H,d], [T,Hkv,d]; views with a contiguous last axis; k may be None),
+    bf16 or fp16, with root-mean-square norms of their heads in front if `eps` is given (weights [d], or None: ones).  freqs [rot/2] fp32
+    (attn_rope_freqs): the rotated dims are offset ... offset + rot - 1, paired i with i + rot/2 or, interleaved, neighbours.
+    positions: int32 [N], [B,N] ([T] for packed tokens), or None: 0 ... N-1.  -> (q_out, k_out), new contiguous tensors unless
+    passed in; an output may be its input."""
+    x = _rows(q, "q", q.dtype, stream)
+    code, dt = _dtype_code(q), q.dtype
+    y = None if k is None else _rows(k, "k", dt, stream, (*q.shape[:-2], k.shape[-2], q.shape[-1]))
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
+    rope = _rope(x, y, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, stream)
+    import torch
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=dt, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=dt, device=q.device)
+    xo = _rows(q_out, "q_out", dt, stream, q.shape)
+    yo = None if k is None else _rows(k_out, "k_out", dt, stream, k.shape)
+    B, N, H, d = x.shape
+    _check(lib().attn_rope_fwd(code, ctypes.byref(rope), x.data_ptr(), _strides(x), _address(y), _strides(y), xo.data_ptr(), _strides(xo),
+                               _address(yo), _strides(yo), B, N, H, 0 if y is None else y.shape[2], d, _stream(stream)))
+    return q_out, k_out
+
+
+def attn_rope_workspace_bytes(B, N, H, Hkv, d) -> int:
+    return int(lib().attn_rope_workspace_bytes(B, N, H, Hkv, d))
+
+
+def attn_rope_bwd(dq, dk, freqs, positions=None, interleaved=False, offset=0, amplitude=1.0, eps=None, q=None, k=None, q_weight=None,
+                  k_weight=None, dq_in=None, dk_in=None, workspace=None, stream=None):
+    """Backward of attn_rope_fwd: dq and dk are the gradients of its outputs (dk None where k was); q and k, its inputs, are needed
+    with norms (eps) only.  -> (dq_in, dk_in, dq_weight, dk_weight): the gradients of q and k, and of the weights in fp32 [d]
+    (None where there are no weights)."""
+    g = _rows(dq, "dq", dq.dtype, stream)
+    code, dt = _dtype_code(dq), dq.dtype
+    h = None if dk is None else _rows(dk, "dk", dt, stream, (*dq.shape[:-2], dk.shape[-2], dq.shape[-1]))
+    x = y = None
+    if eps is not None:
+        if q is None or (k is None) != (dk is None):
+            raise ValueError("with norms the backward pass needs q and k")
+        x = _rows(q, "q", dt, stream, dq.shape)
+        y = None if dk is None else _rows(k, "k", dt, stream, dk.shape)
+    if dk is None and dk_in is not None:
+        raise ValueError("dk_in without dk")
+    rope = _rope(g, h, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, stream)
+    import torch
+    new = lambda like: torch.empty(like.shape, dtype=dt, device=dq.device)
+    dq_in = new(dq) if dq_in is None else dq_in
+    dk_in = new(dk) if dk_in is None and dk is not None else dk_in
+    gi = _rows(dq_in, "dq_in", dt, stream, dq.shape)
+    hi = None if dk is None else _rows(dk_in, "dk_in", dt, stream, dk.shape)
+    B, N, H, d = g.shape
+    Hkv = 0 if h is None else h.shape[2]
+    dqw = None if q_weight is None else torch.empty(d, dtype=torch.float32, device=dq.device)
+    dkw = None if k_weight is None else torch.empty(d, dtype=torch.float32, device=dq.device)
+    if workspace is None:
+        if dqw is not None or dkw is not None:
+            workspace = torch.empty(max(_bytes("attn_rope_workspace_bytes", B, N, H, Hkv, d), 256), dtype=torch.uint8, device=dq.device)
+    else:
+        _here(workspace, "workspace", torch.uint8, stream)
+    _check(lib().attn_rope_bwd(code, ctypes.byref(rope), g.data_ptr(), _strides(g), _address(h), _strides(h), _address(x), _strides(x),
+                               _address(y), _strides(y), gi.data_ptr(), _strides(gi), _address(hi), _strides(hi), _address(dqw), _address(dkw),
+                               B, N, H, Hkv, d, _address(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)))
+    return dq_in, dk_in, dqw, dkw
+
+
+class AttnCache(NamedTuple):
+    """A paged cache in 4 or 8 bits (the formats: include/attn.h): codes k [pages, Hkv, page, d_qk * bits / 8] and v, scale bytes k_scale
+    [pages, Hkv, page, d_qk / 32] and v_scale; uint8, contiguous, on the GPU.  attn_cache_new makes one."""
+    k: object
+    k_scale: object
+    v: object
+    v_scale: object
+
+
+def attn_cache_new(pages, page, Hkv, d_qk, d_v, bits=4, device="cuda"):
+    """A cache of zeros: `pages` pages of `page` tokens (a power of two, 16 ... 65536)."""
+    import torch
+    if bits not in (4, 8):
+        raise ValueError("a cache holds 4 or 8 bits")
+    new = lambda width: torch.zeros(pages, Hkv, page, width, dtype=torch.uint8, device=device)
+    return AttnCache(new(d_qk * bits // 8), new(d_qk // 32), new(d_v * bits // 8), new(d_v // 32))
+
+
+def _cache(cache, stream):
+    import torch
+    lead = cache[0].shape[:3]
+    for t, name in zip(cache, AttnCache._fields):
+        _here(t, "cache." + name, torch.uint8, stream)
+        if t.dim() != 4 or t.shape[:3] != lead or not t.is_contiguous():
+            raise ValueError(f"cache.{name} must be a contiguous uint8 CUDA tensor [pages, Hkv, page, ...]")
+    d = [32 * cache[i].shape[3] for i in (1, 3)]
+    bits = 8 if cache[0].shape[3] == d[0] else 4
+    if cache[0].shape[3] != d[0] * bits // 8 or cache[2].shape[3] != d[1] * bits // 8:
+        raise ValueError("the codes of a cache are as wide as its scales say in 4 or 8 bits")
+    return AttnCacheLayout(*(t.data_ptr() for t in cache), lead[0], lead[2], lead[1], *d, bits)
+
+
+def _indexes(t, name, shape, stream):
+    import torch
+    _here(t, name, torch.int32, stream)
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor {list(shape)}")
+    return t.data_ptr()
+
+
+def attn_cache_write(k, v, slots, cache, stream=None):
+    """Quantises k [T,Hkv,d_qk] and v [T,Hkv,d_v] (bf16 or fp16; views with a contiguous last axis) into slots int32 [T] of the cache
+    (page * tokens-per-page + token in the page; negative or past the cache: the row is skipped; the others all different)."""
+    layout = _cache(cache, stream)
+    code, dt, T = _dtype_code(k), k.dtype, k.shape[0]
+    if k.dim() != 3 or v.dim() != 3:
+        raise ValueError("k and v must be [T, Hkv, d] tensors")
+    x = _rows(k, "k", dt, stream, (T, layout.Hkv, layout.d_qk))
+    y = _rows(v, "v", dt, stream, (T, layout.Hkv, layout.d_v))
+    _check(lib().attn_cache_write(code, ctypes.byref(layout), x.data_ptr(), _strides(x), y.data_ptr(), _strides(y),
+                                  _indexes(slots, "slots", (T,), stream), T, _stream(stream)))
+
+
+def attn_cache_read(slots, cache, dtype, k=None, v=None, stream=None):
+    """The rows at slots int32 [T] as bf16 or fp16 -> (k [T,Hkv,d_qk], v [T,Hkv,d_v]); zeros where a slot is negative or past the cache."""
+    import torch
+    layout = _cache(cache, stream)
+    T = slots.shape[0] if slots.dim() == 1 else 0
+    at = _indexes(slots, "slots", (T,), stream)
+    shapes = [(T, layout.Hkv, layout.d_qk), (T, layout.Hkv, layout.d_v)]
+    k, v = (torch.empty(s, dtype=dtype, device=slots.device) if t is None else t for t, s in zip((k, v), shapes))
+    code = _dtype_code(k)
+    for t, name, s in zip((k, v), "kv", shapes):
+        _here(t, name, dtype, stream)
+        _dev(t, name, s, dtype)
+    _check(lib().attn_cache_read(code, ctypes.byref(layout), at, T, k.data_ptr(), v.data_ptr(), _stream(stream)))
+    return k, v
+
+
+def attn_cache_workspace_bytes(cache, B, Nq, H, table_width) -> int:
+    return int(lib().attn_cache_workspace_bytes(ctypes.byref(_cache(cache, None)), B, Nq, H, table_width))
+
+
+def attn_cache_fwd(q, cache, block_table, lens, scale, causal, o=None, lse=None, workspace=None, stream=None):
+    """Attention of q [B,Nq,H,d_qk] (a view with a contiguous last axis) over a paged cache: sequence b has lens[b] keys (int32 [B]), key j
+    in page block_table[b, j // page] (int32 [B,width]); under the causal mask the last query sees the last key.
+    -> (o [B,Nq,H,d_v], lse [B,H,Nq] fp32); a query without a visible key has o = 0 and lse = -inf."""
+    import torch
+    layout = _cache(cache, stream)
+    code, dt = _dtype_code(q), q.dtype
+    if q.dim() != 4:
+        raise ValueError("q must be a [B, Nq, H, d] tensor")
+    B, Nq, H, d = q.shape
+    x = _rows(q, "q", dt, stream, (B, Nq, H, layout.d_qk))
+    width = block_table.shape[1] if block_table.dim() == 2 else 0
+    table, keys = _indexes(block_table, "block_table", (B, width), stream), _indexes(lens, "lens", (B,), stream)
+    if o is None:
+        o = torch.empty((B, Nq, H, layout.d_v), dtype=dt, device=q.device)
+    if lse is None:
+        lse = torch.empty((B, H, Nq), dtype=torch.float32, device=q.device)
+    y = _rows(o, "o", dt, stream, (B, Nq, H, layout.d_v))
+    _here(lse, "lse", torch.float32, stream)
+    lse_p = _dev_lse(lse, (B, H, Nq), "B,H,Nq")
+    if workspace is None:
+        need = lib().attn_cache_workspace_bytes(ctypes.byref(layout), B, Nq, H, width)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    else:
+        _here(workspace, "workspace", torch.uint8, stream)
+    _check(lib().attn_cache_fwd(code, ctypes.byref(layout), x.data_ptr(), _strides(x), y.data_ptr(), _strides(y), lse_p, table, width, keys,
+                                B, Nq, H, float(scale), int(bool(causal)), workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    return o, lse

@@ -36,6 +36,9 @@ SOURCES = [*[("attn_bwd_dq_q64.hip", f"attn_bwd_dq_q64_{f16}{varlen}.o", [f"-DAT
            ("attn_bwd.hip", "attn_bwd_vgpr_form.o", ["-DATTN_BWD_VGPR_FORM_PART=1", *VGPR_FORM]),
            ("attn_bwd_short.hip", "attn_bwd_short.o", []),
            ("attn_varlen.hip", "attn_varlen.o", []),
+           ("attn_rope.hip", "attn_rope.o", []),
+           ("attn_cache.hip", "attn_cache.o", []),
+           *[("attn_cache_fwd.hip", f"attn_cache_fwd_{f16}.o", [f"-DATTN_F16={f16}", *VGPR_FORM]) for f16 in (0, 1)],
            ("exp2_emulated.hip", "exp2_emulated.o", [])]
 PROBE_SOURCES = [("probes.hip", "probes.o", [])]
 # packed-fp32 instruction selection is switched off on purpose (device passes only; the

@@ -2,6 +2,7 @@
 // See include/attn.h for the contract of every entry point.
 #include "../../include/attn.h"
 #include "launch.h"
+#include "ops.h"
 
 #include <stdint.h>
 
@@ -515,6 +516,256 @@ int attn_bwd_strided(int dtype, const void* q, const attn_strides_t* sq, const v
                           scale, causal, ws + 2 * cu_bytes(B), st, Nq, stream);
 }
 
+// ---------------------------------------------------------------------------------------------
+// rotary positions and head norms
+
+namespace {
+
+int check_rope(int dtype, const attn_rope_t* r, bool k, int B, int N, int H, int Hkv, int d)
+{
+    if (dtype != ATTN_BF16 && dtype != ATTN_F16) return ATTN_EUNSUPPORTED;
+    if (!r || !r->freqs || B <= 0 || N <= 0 || H <= 0 || (k && Hkv <= 0)) return ATTN_EINVAL;
+    if (d != 64 && d != 96 && d != 128 && d != 192 && d != 256) return ATTN_EUNSUPPORTED;
+    if (r->rot <= 0 || r->offset < 0 || r->rot > d || r->offset > d - r->rot || r->positions_batch < 0) return ATTN_EINVAL;
+    if (!(r->amplitude > -1e30f && r->amplitude < 1e30f)) return ATTN_EINVAL;
+    if (r->norm ? !(r->eps >= 0.0f && r->eps < 1e30f) : r->q_weight || r->k_weight) return ATTN_EINVAL;
+    if (!k && r->k_weight) return ATTN_EINVAL;
+    if (misaligned(r->freqs, 4) || misaligned(r->positions, 4) || misaligned(r->q_weight, 16) || misaligned(r->k_weight, 16)) return ATTN_EINVAL;
+    if (r->rot % 16 || r->offset % 8) return ATTN_EUNSUPPORTED;
+    if ((int64_t)B * N > (1 << 30) || (int64_t)H + (k ? Hkv : 0) > (1 << 20)) return ATTN_EUNSUPPORTED;
+    return ATTN_OK;
+}
+
+attn::Stride3 as_is(const attn_strides_t* s) { return s ? attn::Stride3{s->batch, s->row, s->head} : attn::Stride3{0, 0, 0}; }
+
+attn::RopeArgs rope_args(int dtype, const attn_rope_t* r, int B, int N, int H, int Hkv, int d, void* stream)
+{
+    attn::RopeArgs a = {};
+    a.w[0] = r->q_weight;
+    a.w[1] = r->k_weight;
+    a.heads[0] = H;
+    a.heads[1] = Hkv;
+    a.freqs = r->freqs;
+    a.positions = r->positions;
+    a.positions_batch = r->positions_batch;
+    a.B = B;
+    a.N = N;
+    a.d = d;
+    a.rot = r->rot;
+    a.offset = r->offset;
+    a.amplitude = r->amplitude;
+    a.sign = 1.0f;
+    a.eps = r->eps;
+    a.interleaved = r->interleaved != 0;
+    a.norm = r->norm != 0;
+    a.f16 = dtype == ATTN_F16;
+    a.stream = stream;
+    return a;
+}
+
+}  // namespace
+
+int attn_rope_fwd(int dtype, const attn_rope_t* rope, const void* q, const attn_strides_t* sq, const void* k, const attn_strides_t* sk,
+                  void* q_out, const attn_strides_t* sqo, void* k_out, const attn_strides_t* sko,
+                  int B, int N, int H, int Hkv, int d, void* stream)
+{
+    const bool both = k != nullptr;
+    if (int rc = check_rope(dtype, rope, both, B, N, H, Hkv, d)) return rc;
+    if (!q || !q_out || both != (k_out != nullptr)) return ATTN_EINVAL;
+    if (misaligned(q, 16) || misaligned(k, 16) || misaligned(q_out, 16) || misaligned(k_out, 16)) return ATTN_EINVAL;
+    if (bad_stride(sq, B, N, H) || bad_stride(sqo, B, N, H)) return ATTN_EINVAL;
+    if (both && (bad_stride(sk, B, N, Hkv) || bad_stride(sko, B, N, Hkv))) return ATTN_EINVAL;
+    attn::RopeArgs a = rope_args(dtype, rope, B, N, H, both ? Hkv : 0, d, stream);
+    a.x[0] = q;
+    a.x[1] = k;
+    a.y[0] = q_out;
+    a.y[1] = k_out;
+    a.sx[0] = as_is(sq);
+    a.sx[1] = as_is(both ? sk : nullptr);
+    a.sy[0] = as_is(sqo);
+    a.sy[1] = as_is(both ? sko : nullptr);
+    return attn::launch_rope(a) == 0 ? ATTN_OK : ATTN_ELAUNCH;
+}
+
+size_t attn_rope_workspace_bytes(int B, int N, int H, int Hkv, int d)
+{
+    if (B <= 0 || N <= 0 || H <= 0 || Hkv < 0 || (int64_t)B * N > (1 << 30) || (int64_t)H + Hkv > (1 << 20)) return 0;
+    if (d != 64 && d != 96 && d != 128 && d != 192 && d != 256) return 0;
+    return align_up((size_t)attn::rope_shape(B * N, H + Hkv, d, true).blocks * 2 * d * sizeof(float), 256);
+}
+
+int attn_rope_bwd(int dtype, const attn_rope_t* rope, const void* dq, const attn_strides_t* sdq, const void* dk, const attn_strides_t* sdk,
+                  const void* q, const attn_strides_t* sq, const void* k, const attn_strides_t* sk,
+                  void* dq_in, const attn_strides_t* sdqi, void* dk_in, const attn_strides_t* sdki, float* dq_weight, float* dk_weight,
+                  int B, int N, int H, int Hkv, int d, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const bool both = dk != nullptr;
+    if (int rc = check_rope(dtype, rope, both, B, N, H, Hkv, d)) return rc;
+    const bool norm = rope->norm != 0, sums = dq_weight || dk_weight;
+    if (!dq || !dq_in || both != (dk_in != nullptr)) return ATTN_EINVAL;
+    if (norm && (!q || both != (k != nullptr))) return ATTN_EINVAL;
+    if ((dq_weight && !rope->q_weight) || (dk_weight && !rope->k_weight)) return ATTN_EINVAL;
+    const void* ptrs[] = {dq, dk, q, k, dq_in, dk_in};
+    for (const void* p : ptrs)
+        if (misaligned(p, 16)) return ATTN_EINVAL;
+    if (misaligned(dq_weight, 4) || misaligned(dk_weight, 4) || misaligned(workspace, 256)) return ATTN_EINVAL;
+    if (bad_stride(sdq, B, N, H) || bad_stride(sdqi, B, N, H) || (norm && bad_stride(sq, B, N, H))) return ATTN_EINVAL;
+    if (both && (bad_stride(sdk, B, N, Hkv) || bad_stride(sdki, B, N, Hkv) || (norm && bad_stride(sk, B, N, Hkv)))) return ATTN_EINVAL;
+    if (sums && (!workspace || workspace_bytes < attn_rope_workspace_bytes(B, N, H, both ? Hkv : 0, d))) return ATTN_EINVAL;
+    attn::RopeArgs a = rope_args(dtype, rope, B, N, H, both ? Hkv : 0, d, stream);
+    a.sign = -1.0f;
+    a.y[0] = dq_in;
+    a.y[1] = dk_in;
+    a.sy[0] = as_is(sdqi);
+    a.sy[1] = as_is(both ? sdki : nullptr);
+    if (norm) {
+        a.backward = true;
+        a.x[0] = q;
+        a.x[1] = k;
+        a.sx[0] = as_is(sq);
+        a.sx[1] = as_is(both ? sk : nullptr);
+        a.dy[0] = dq;
+        a.dy[1] = dk;
+        a.sdy[0] = as_is(sdq);
+        a.sdy[1] = as_is(both ? sdk : nullptr);
+        a.dw[0] = dq_weight;
+        a.dw[1] = dk_weight;
+        a.part = sums ? static_cast<float*>(workspace) : nullptr;
+    } else {                                               // the rotation back is a forward pass by the opposite angles
+        a.x[0] = dq;
+        a.x[1] = dk;
+        a.sx[0] = as_is(sdq);
+        a.sx[1] = as_is(both ? sdk : nullptr);
+    }
+    return attn::launch_rope(a) == 0 ? ATTN_OK : ATTN_ELAUNCH;
+}
+
+// ---------------------------------------------------------------------------------------------
+// the quantised cache
+
+namespace {
+
+int check_cache(const attn_cache_t* c)
+{
+    if (!c || !c->k || !c->k_scale || !c->v || !c->v_scale || c->pages <= 0 || c->page <= 0 || c->Hkv <= 0) return ATTN_EINVAL;
+    if (misaligned(c->k, 16) || misaligned(c->v, 16)) return ATTN_EINVAL;
+    if (!dims_supported(c->d_qk, c->d_v) || (c->bits != 4 && c->bits != 8)) return ATTN_EUNSUPPORTED;
+    if (c->page < 16 || c->page > 65536 || (c->page & (c->page - 1))) return ATTN_EUNSUPPORTED;
+    if ((int64_t)c->pages * c->page > 0x7fffffffLL || c->Hkv > 65536) return ATTN_EUNSUPPORTED;
+    return ATTN_OK;
+}
+
+attn::CacheArgs cache_args(const attn_cache_t* c)
+{
+    return {c->k, c->k_scale, c->v, c->v_scale, c->pages, __builtin_ctz((unsigned)c->page), c->Hkv, c->d_qk, c->d_v, c->bits};
+}
+
+int check_cache_rows(int dtype, const attn_cache_t* c, const int* slots, int T)
+{
+    if (dtype != ATTN_BF16 && dtype != ATTN_F16) return ATTN_EUNSUPPORTED;
+    if (int rc = check_cache(c)) return rc;
+    if (!slots || T <= 0 || misaligned(slots, 4)) return ATTN_EINVAL;
+    const int64_t chunks = (int64_t)T * c->Hkv * ((c->d_qk > c->d_v ? c->d_qk : c->d_v) / 8);
+    return (chunks + 255) / 256 > 0x7fffffffLL ? ATTN_EUNSUPPORTED : ATTN_OK;
+}
+
+int check_cache_fwd(const attn_cache_t* c, int B, int Nq, int H, int table_width)
+{
+    if (int rc = check_cache(c)) return rc;
+    if (B <= 0 || Nq <= 0 || H <= 0 || table_width <= 0 || H % c->Hkv != 0) return ATTN_EINVAL;
+    const int64_t most = (int64_t)table_width * c->page;
+    if (most > 0x7fffffffLL - 31 || B * ((most + 31) / 32) > (1 << 30)) return ATTN_EUNSUPPORTED;
+    if ((int64_t)Nq * H > (1 << 24) || (int64_t)B * Nq * H > 0x7fffffffLL) return ATTN_EUNSUPPORTED;
+    const attn::CacheShape s = attn::cache_shape(B, Nq, H, c->Hkv, most);
+    return (int64_t)s.slots * Nq * H > 0x7fffffffLL ? ATTN_EUNSUPPORTED : ATTN_OK;
+}
+
+// partial results of every chunk, if there can be more than one to a sequence
+size_t cache_parts(const attn_cache_t* c, int B, int Nq, int H, int table_width)
+{
+    const attn::CacheShape s = attn::cache_shape(B, Nq, H, c->Hkv, (int64_t)table_width * c->page);
+    return s.slots > B ? (size_t)s.slots * Nq * H : 0;
+}
+
+}  // namespace
+
+int attn_cache_write(int dtype, const attn_cache_t* cache, const void* k, const attn_strides_t* sk, const void* v, const attn_strides_t* sv,
+                     const int* slots, int T, void* stream)
+{
+    if (int rc = check_cache_rows(dtype, cache, slots, T)) return rc;
+    if (!k || !v || misaligned(k, 16) || misaligned(v, 16)) return ATTN_EINVAL;
+    if (bad_stride(sk, 1, T, cache->Hkv) || bad_stride(sv, 1, T, cache->Hkv)) return ATTN_EINVAL;
+    attn::CacheRowsArgs a = {};
+    a.c = cache_args(cache);
+    a.xk = k;
+    a.xv = v;
+    a.k_row = sk->row;
+    a.k_head = sk->head;
+    a.v_row = sv->row;
+    a.v_head = sv->head;
+    a.slots = slots;
+    a.T = T;
+    a.f16 = dtype == ATTN_F16;
+    a.stream = stream;
+    return attn::launch_cache_write(a) == 0 ? ATTN_OK : ATTN_ELAUNCH;
+}
+
+int attn_cache_read(int dtype, const attn_cache_t* cache, const int* slots, int T, void* k, void* v, void* stream)
+{
+    if (int rc = check_cache_rows(dtype, cache, slots, T)) return rc;
+    if (!k || !v || misaligned(k, 16) || misaligned(v, 16)) return ATTN_EINVAL;
+    attn::CacheRowsArgs a = {};
+    a.c = cache_args(cache);
+    a.yk = k;
+    a.yv = v;
+    a.slots = slots;
+    a.T = T;
+    a.f16 = dtype == ATTN_F16;
+    a.stream = stream;
+    return attn::launch_cache_read(a) == 0 ? ATTN_OK : ATTN_ELAUNCH;
+}
+
+size_t attn_cache_workspace_bytes(const attn_cache_t* cache, int B, int Nq, int H, int table_width)
+{
+    if (check_cache_fwd(cache, B, Nq, H, table_width) != ATTN_OK) return 0;
+    return align_up(cache_parts(cache, B, Nq, H, table_width) * (cache->d_v + 2) * sizeof(float) + 1, 256);
+}
+
+int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, void* o, const attn_strides_t* so, float* lse,
+                   const int* block_table, int table_width, const int* lens, int B, int Nq, int H, float scale, int causal,
+                   void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (dtype != ATTN_BF16 && dtype != ATTN_F16) return ATTN_EUNSUPPORTED;
+    if (!q || !o || !lse || !block_table || !lens || !workspace) return ATTN_EINVAL;
+    if (int rc = check_cache_fwd(cache, B, Nq, H, table_width)) return rc;
+    if (bad_stride(sq, B, Nq, H) || bad_stride(so, B, Nq, H)) return ATTN_EINVAL;
+    if (!(scale > 0.0f) || !(scale < 1e30f)) return ATTN_EINVAL;
+    if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4) || misaligned(block_table, 4) || misaligned(lens, 4) || misaligned(workspace, 256))
+        return ATTN_EINVAL;
+    if (workspace_bytes < attn_cache_workspace_bytes(cache, B, Nq, H, table_width)) return ATTN_EINVAL;
+    attn::CacheFwdArgs a = {};
+    a.c = cache_args(cache);
+    a.q = q;
+    a.o = o;
+    a.lse = lse;
+    a.sq = as_is(sq);
+    a.so = as_is(so);
+    a.table = block_table;
+    a.lens = lens;
+    a.table_width = table_width;
+    a.B = B;
+    a.Nq = Nq;
+    a.H = H;
+    a.scale = scale;
+    a.causal = causal != 0;
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = a.part_o + cache_parts(cache, B, Nq, H, table_width) * cache->d_v;
+    a.f16 = dtype == ATTN_F16;
+    a.stream = stream;
+    const int rc = attn::launch_cache_fwd(a);
+    return rc == 0 ? ATTN_OK : (rc == -2 ? ATTN_EUNSUPPORTED : ATTN_ELAUNCH);
+}
+
 const char* attn_strerror(int code)
 {
     switch (code) {
@@ -522,7 +773,8 @@ const char* attn_strerror(int code)
         case ATTN_EINVAL: return "invalid argument (null or misaligned pointer, bad size, H % Hkv != 0, "
                                  "non-positive scale, or workspace too small)";
         case ATTN_EUNSUPPORTED: return "unsupported shape: (d_qk, d_v) must be (64,64), (96,96), (128,128), "
-                                       "(192,128) or (256,256) and N a multiple of 128";
+                                       "(192,128) or (256,256) and N a multiple of 128; a rotated part 16 n dims from 8 m on; "
+                                       "a cache in 4 or 8 bits, its pages of 16 ... 65536 tokens, a power of two";
         case ATTN_ELAUNCH: return "HIP kernel launch failed";
         case ATTN_ETOOLARGE: return "B * H * N exceeds ATTN_NOALLOC_MAX_ROWS, the size of the built-in workspace of "
                                     "attn_bwd_noalloc: use attn_bwd_ex with a workspace of your own";

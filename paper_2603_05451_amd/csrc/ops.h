@@ -1,0 +1,121 @@
+// Host-side argument bundles of the rotary and cache calls, as launch.h has them for the attention calls, and the rules that
+// share their work out (arithmetic on sizes alone, without HIP for a host compiler).
+#pragma once
+#include <stdint.h>
+
+namespace attn {
+
+// ---- rotary positions and head norms
+
+// Lanes of a wave that hold one row: two chunks of 8 dims each, a power of two.
+inline int rope_lanes(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
+
+struct RopeShape {
+    int blocks;         // of four waves
+    int hg_shift;       // heads of a token side by side in a wave: 2^hg_shift
+    int shares;         // blocks that divide the heads of a group of tokens
+};
+inline RopeShape rope_shape(int tokens, int heads, int d, bool sums)
+{
+    const int slots = 64 / rope_lanes(d), turn = sums ? 2 : 4;
+    RopeShape r{0, 0, 1};
+    auto waves = [&] { return ((int64_t)tokens * (1 << r.hg_shift) + slots - 1) / slots; };
+    while (waves() < 8192 && (1 << r.hg_shift) < slots && (1 << r.hg_shift) < heads) ++r.hg_shift;
+    const int turns = (heads + (turn << r.hg_shift) - 1) / (turn << r.hg_shift);
+    if (waves() < 2048) r.shares = turns;
+    int64_t groups = (waves() + 3) / 4;
+    if (sums && groups * r.shares > 1024) groups = (1024 + r.shares - 1) / r.shares;
+    r.blocks = (int)(groups * r.shares);
+    return r;
+}
+
+// ---- attention over the cache
+
+// Blocks of 16 rows that a wave takes together: two where there are more than 16 rows (queries times heads of a group).
+inline int cache_row_blocks(int Nq, int H, int Hkv) { return (int64_t)Nq * (H / Hkv) > 16 ? 2 : 1; }
+
+struct CacheShape {
+    int parts;          // chunks that the keys of all sequences are divided into, about
+    int min_tiles;      // a chunk has at least so many 32-key tiles
+    int slots;          // chunks at most: one per sequence more than `parts`, or what the longest sequences could have
+};
+inline CacheShape cache_shape(int B, int Nq, int H, int Hkv, int64_t most)
+{
+    const int64_t rows = (int64_t)Nq * (H / Hkv), per = 16 * cache_row_blocks(Nq, H, Hkv);
+    const int64_t side = Hkv * ((rows + per - 1) / per);           // blocks per chunk
+    CacheShape s;
+    s.parts = (int)(side < 1024 ? 1024 / side : 1);
+    s.min_tiles = 8;
+    const int64_t tiles = (most + 31) / 32, each = (tiles + s.min_tiles - 1) / s.min_tiles;
+    s.slots = (int)(B * each < (int64_t)s.parts + B ? B * (each ? each : 1) : s.parts + B);
+    return s;
+}
+
+}  // namespace attn
+
+#if defined(__HIP__)
+#include "launch.h"
+
+namespace attn {
+
+struct RopeArgs {
+    const void* x[2];           // q, k (null where there is none, heads 0)
+    const void* dy[2];          // backward pass: gradients of the outputs
+    void* y[2];                 // outputs; backward pass: gradients of x
+    Stride3 sx[2], sdy[2], sy[2];
+    const void* w[2];           // weights of the norms, or null: ones
+    float* dw[2];               // their gradients, or null
+    float* part;                // partial sums of those: [blocks][2][d]
+    int heads[2];
+    const float* freqs;
+    const int* positions;       // or null: 0, 1, ... in every sequence
+    long long positions_batch;
+    int B, N, d, rot, offset;
+    float amplitude, sign, eps;
+    bool interleaved, norm, backward, f16;
+    void* stream;
+    int hg_shift, shares, units;     // rope_shape's (launch_rope sets them)
+};
+int launch_rope(RopeArgs a);
+
+// ---- the quantised cache
+
+struct CacheArgs {
+    void *k, *k_scale, *v, *v_scale;
+    int pages, page_shift, Hkv, d_qk, d_v, bits;
+};
+
+struct CacheRowsArgs {          // writing (rows in x) and reading (rows in y, dense)
+    CacheArgs c;
+    const void *xk, *xv;
+    long long k_row, k_head, v_row, v_head;
+    void *yk, *yv;
+    const int* slots;
+    int T;
+    bool f16;
+    void* stream;
+};
+int launch_cache_write(const CacheRowsArgs& a);
+int launch_cache_read(const CacheRowsArgs& a);
+
+struct CacheFwdArgs {
+    CacheArgs c;
+    const void* q;
+    void* o;
+    float* lse;
+    Stride3 sq, so;
+    const int *table, *lens;
+    int table_width;
+    int B, Nq, H;
+    float scale;
+    int causal;
+    float *part_o, *part_ml;    // unnormalised results of chunks: [slots][Hkv][Nq * H / Hkv][d_v], and {maximum, sum} of each row
+    bool f16;
+    void* stream;
+};
+int launch_cache_fwd_bf16(const CacheFwdArgs& a);       // one object each
+int launch_cache_fwd_f16(const CacheFwdArgs& a);
+inline int launch_cache_fwd(const CacheFwdArgs& a) { return a.f16 ? launch_cache_fwd_f16(a) : launch_cache_fwd_bf16(a); }
+
+}  // namespace attn
+#endif
