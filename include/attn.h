@@ -307,7 +307,7 @@ int attn_rope_bwd(int dtype, const attn_rope_t* rope, const void* dq, const attn
  * of the block is cut off when it is rounded to nearest (ties to even); a block that holds an infinity or a NaN is NaN.  Rounding
  * is exact arithmetic: codes and scales depend on the row's values alone.
  *   page: tokens per page, a power of two, 16 ... 65536; pages * page <= 2^31 - 1; head dims as elsewhere.
- * Slot s is token s % page of page s / page. */
+ * Slot s is token s % page of page s / page.  Calls on rows take T * Hkv * d up to 2^34 - 2048. */
 typedef struct attn_cache {
     void *k, *k_scale, *v, *v_scale;
     int pages, page, Hkv, d_qk, d_v, bits;

@@ -591,7 +591,9 @@ size_t attn_rope_workspace_bytes(int B, int N, int H, int Hkv, int d)
 {
     if (B <= 0 || N <= 0 || H <= 0 || Hkv < 0 || (int64_t)B * N > (1 << 30) || (int64_t)H + Hkv > (1 << 20)) return 0;
     if (d != 64 && d != 96 && d != 128 && d != 192 && d != 256) return 0;
-    return align_up((size_t)attn::rope_shape(B * N, H + Hkv, d, true).blocks * 2 * d * sizeof(float), 256);
+    attn::RopeShape shape[2];
+    attn::rope_shapes(B * N, H, Hkv, d, true, shape);
+    return align_up((size_t)(shape[0].blocks + shape[1].blocks) * d * sizeof(float), 256);
 }
 
 int attn_rope_bwd(int dtype, const attn_rope_t* rope, const void* dq, const attn_strides_t* sdq, const void* dk, const attn_strides_t* sdk,
@@ -666,7 +668,7 @@ int check_cache_rows(int dtype, const attn_cache_t* c, const int* slots, int T)
     if (int rc = check_cache(c)) return rc;
     if (!slots || T <= 0 || misaligned(slots, 4)) return ATTN_EINVAL;
     const int64_t chunks = (int64_t)T * c->Hkv * ((c->d_qk > c->d_v ? c->d_qk : c->d_v) / 8);
-    return (chunks + 255) / 256 > 0x7fffffffLL ? ATTN_EUNSUPPORTED : ATTN_OK;
+    return chunks > 0x7fffff00LL ? ATTN_EUNSUPPORTED : ATTN_OK;
 }
 
 int check_cache_fwd(const attn_cache_t* c, int B, int Nq, int H, int table_width)
@@ -676,14 +678,14 @@ int check_cache_fwd(const attn_cache_t* c, int B, int Nq, int H, int table_width
     const int64_t most = (int64_t)table_width * c->page;
     if (most > 0x7fffffffLL - 31 || B * ((most + 31) / 32) > (1 << 30)) return ATTN_EUNSUPPORTED;
     if ((int64_t)Nq * H > (1 << 24) || (int64_t)B * Nq * H > 0x7fffffffLL) return ATTN_EUNSUPPORTED;
-    const attn::CacheShape s = attn::cache_shape(B, Nq, H, c->Hkv, most);
+    const attn::CacheShape s = attn::cache_shape(B, Nq, H, c->Hkv, c->d_qk, c->bits, most);
     return (int64_t)s.slots * Nq * H > 0x7fffffffLL ? ATTN_EUNSUPPORTED : ATTN_OK;
 }
 
 // partial results of every chunk, if there can be more than one to a sequence
 size_t cache_parts(const attn_cache_t* c, int B, int Nq, int H, int table_width)
 {
-    const attn::CacheShape s = attn::cache_shape(B, Nq, H, c->Hkv, (int64_t)table_width * c->page);
+    const attn::CacheShape s = attn::cache_shape(B, Nq, H, c->Hkv, c->d_qk, c->bits, (int64_t)table_width * c->page);
     return s.slots > B ? (size_t)s.slots * Nq * H : 0;
 }
 

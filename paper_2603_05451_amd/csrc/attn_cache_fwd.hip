@@ -34,22 +34,21 @@ struct CachePlace {
     int b, len, chunk, chunks, chunk_tiles;     // of a sequence; chunks of chunk_tiles 32-key tiles
 };
 
-__device__ __forceinline__ int wave_sum(int x)
+// Inclusive prefix sums over the lanes of a wave: within 16 lanes, then the ends of rows 0 and 2 to rows 1 and 3, then that of row 1 to
+// both upper rows.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_moved(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_prefix(int x)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
-    return x;
+    x = add_moved<0x111, 0xf>(x);          // row_shr 1, 2, 4, 8
+    x = add_moved<0x112, 0xf>(x);
+    x = add_moved<0x114, 0xf>(x);
+    x = add_moved<0x118, 0xf>(x);
+    x = add_moved<0x142, 0xa>(x);          // row_bcast 15
+    return add_moved<0x143, 0xc>(x);       // row_bcast 31
 }
-__device__ __forceinline__ int wave_prefix(int x)       // inclusive
-{
-    const int l = threadIdx.x & 63;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const int y = __shfl_up(x, m);
-        x += l >= m ? y : 0;
-    }
-    return x;
-}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
+
 // Keys of sequence b as the kernels take them: no more than its row of the table has room for, none if the length is negative.
 __device__ __forceinline__ int cache_length(const CachePlanArgs& p, const int* __restrict__ lens, int b)
 {
@@ -61,46 +60,64 @@ __device__ __forceinline__ int cache_chunk_tiles(const CachePlanArgs& p, const i
     int total = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) total += (cache_length(p, lens, b0 + (threadIdx.x & 63)) + 31) >> 5;
     total = wave_sum(total);
-    return __builtin_amdgcn_readfirstlane(max(((total + p.parts - 1) / p.parts + 3) & ~3, p.min_tiles));
+    return max(((total + p.parts - 1) / p.parts + 3) & ~3, p.min_tiles);
 }
-__device__ __forceinline__ int cache_chunks(int len, int chunk_tiles) { return max(1, (((len + 31) >> 5) + chunk_tiles - 1) / chunk_tiles); }
+// The chunks of a sequence: whole ones, and one that is shorter (also if there are no keys, for its rows have results).
+struct CacheSplit {
+    int whole, rest;
+};
+__device__ __forceinline__ CacheSplit cache_split(int len, int chunk_tiles)
+{
+    const int tiles = (len + 31) >> 5, whole = tiles / chunk_tiles;
+    return {whole, tiles > whole * chunk_tiles || tiles == 0};
+}
 
-// The sequence and chunk at place `slot` of all chunks, the sequences' in order; false behind the last one.
+// The sequence and chunk at place `slot` of all chunks: the whole ones of all sequences, in order, then the shorter ones, so that
+// these fill up what the others leave.  False behind the last one.
 __device__ __forceinline__ bool cache_place(const CachePlanArgs& p, const int* __restrict__ lens, int slot, CachePlace& at)
 {
     at.chunk_tiles = cache_chunk_tiles(p, lens);
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int b = b0 + (threadIdx.x & 63);
-        const int len = cache_length(p, lens, b);
-        const int n = b < p.B ? cache_chunks(len, at.chunk_tiles) : 0;
-        const int upto = wave_prefix(n);
-        const uint64_t past = __ballot(upto > slot);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            at.b = b0 + l;
-            at.len = __builtin_amdgcn_readlane(len, l);
-            at.chunks = __builtin_amdgcn_readlane(n, l);
-            at.chunk = slot - (__builtin_amdgcn_readlane(upto, l) - at.chunks);
-            return true;
+    for (int pass = 0; pass < 2; ++pass)
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            const int b = b0 + (threadIdx.x & 63);
+            const int len = cache_length(p, lens, b);
+            const CacheSplit split = b < p.B ? cache_split(len, at.chunk_tiles) : CacheSplit{0, 0};
+            const int n = pass ? split.rest : split.whole;
+            const int upto = wave_prefix(n);
+            const uint64_t past = __ballot(upto > slot);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+                at.b = b0 + l;
+                at.len = of(len);
+                at.chunks = of(split.whole + split.rest);
+                at.chunk = pass ? of(split.whole) : slot - (of(upto) - of(n));
+                return true;
+            }
+            slot -= __builtin_amdgcn_readlane(upto, 63);
         }
-        slot -= __builtin_amdgcn_readlane(upto, 63);
-    }
     return false;
 }
-// The place of sequence b's first chunk.
-__device__ __forceinline__ void cache_place_of(const CachePlanArgs& p, const int* __restrict__ lens, int b, CachePlace& at, int& slot0)
+// The places of sequence b's first whole chunk and of its shorter one (if there is one).
+__device__ __forceinline__ void cache_place_of(const CachePlanArgs& p, const int* __restrict__ lens, int b, CachePlace& at, int& slot0, int& rest)
 {
     at.b = b;
     at.chunk_tiles = cache_chunk_tiles(p, lens);
-    at.len = cache_length(p, lens, b);
-    at.chunks = __builtin_amdgcn_readfirstlane(cache_chunks(at.len, at.chunk_tiles));
     at.chunk = 0;
-    int before = 0;
-    for (int b0 = 0; b0 < b; b0 += 64) {
+    int whole = 0, before = 0, rests = 0, len = 0;      // whole chunks of all, those before b, shorter ones before b
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
         const int i = b0 + (threadIdx.x & 63);
-        if (i < b) before += cache_chunks(cache_length(p, lens, i), at.chunk_tiles);
+        const int n = cache_length(p, lens, i);
+        const CacheSplit split = i < p.B ? cache_split(n, at.chunk_tiles) : CacheSplit{0, 0};
+        whole += split.whole;
+        if (i < b) { before += split.whole; rests += split.rest; }
+        if (i == b) len = n;
     }
-    slot0 = __builtin_amdgcn_readfirstlane(wave_sum(before));
+    at.len = wave_sum(len);
+    const CacheSplit mine = cache_split(at.len, at.chunk_tiles);
+    at.chunks = mine.whole + mine.rest;
+    slot0 = wave_sum(before);
+    rest = mine.rest ? wave_sum(whole) + wave_sum(rests) : -1;
 }
 
 #if ATTN_F16

@@ -10,23 +10,34 @@ namespace attn {
 // Lanes of a wave that hold one row: two chunks of 8 dims each, a power of two.
 inline int rope_lanes(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 
+// Rows of a lane whose loads are in flight together.
+constexpr int rope_rows(bool backward) { return backward ? 2 : 4; }
+
 struct RopeShape {
     int blocks;         // of four waves
     int hg_shift;       // heads of a token side by side in a wave: 2^hg_shift
     int shares;         // blocks that divide the heads of a group of tokens
 };
-inline RopeShape rope_shape(int tokens, int heads, int d, bool sums)
+// How the rows of one tensor are shared out.  A lane goes through as many heads of its token as there are waves to spare for: that
+// many rows share their angles.
+inline RopeShape rope_shape(int tokens, int heads, int d, bool backward)
 {
-    const int slots = 64 / rope_lanes(d), turn = sums ? 2 : 4;
+    const int slots = 64 / rope_lanes(d), rows = rope_rows(backward);
     RopeShape r{0, 0, 1};
     auto waves = [&] { return ((int64_t)tokens * (1 << r.hg_shift) + slots - 1) / slots; };
-    while (waves() < 8192 && (1 << r.hg_shift) < slots && (1 << r.hg_shift) < heads) ++r.hg_shift;
-    const int turns = (heads + (turn << r.hg_shift) - 1) / (turn << r.hg_shift);
-    if (waves() < 2048) r.shares = turns;
+    while (waves() < 1024 && (1 << r.hg_shift) < slots && (1 << r.hg_shift) < heads) ++r.hg_shift;
+    const int turns = (heads + (rows << r.hg_shift) - 1) / (rows << r.hg_shift);
+    if (waves() < 1024) r.shares = turns;
     int64_t groups = (waves() + 3) / 4;
-    if (sums && groups * r.shares > 1024) groups = (1024 + r.shares - 1) / r.shares;
+    if (backward && groups * r.shares > 512) groups = (512 + r.shares - 1) / r.shares;      // partial sums per block
     r.blocks = (int)(groups * r.shares);
     return r;
+}
+// q and k (heads_k = 0: there is none)
+inline void rope_shapes(int tokens, int heads_q, int heads_k, int d, bool backward, RopeShape (&shape)[2])
+{
+    shape[0] = rope_shape(tokens, heads_q, d, backward);
+    shape[1] = heads_k > 0 ? rope_shape(tokens, heads_k, d, backward) : RopeShape{0, 0, 1};
 }
 
 // ---- attention over the cache
@@ -34,17 +45,24 @@ inline RopeShape rope_shape(int tokens, int heads, int d, bool sums)
 // Blocks of 16 rows that a wave takes together: two where there are more than 16 rows (queries times heads of a group).
 inline int cache_row_blocks(int Nq, int H, int Hkv) { return (int64_t)Nq * (H / Hkv) > 16 ? 2 : 1; }
 
+// Blocks of the attention kernel that a CU holds: what its registers allow (the kernel is compiled for it).
+constexpr int cache_blocks_per_cu(int d_qk, int bits, int row_blocks)
+{
+    return d_qk > 192 ? 1 : d_qk > 128 ? (bits == 8 && row_blocks == 2 ? 1 : 2) : d_qk > 64 ? (bits == 4 && row_blocks == 1 ? 3 : 2) : row_blocks == 1 ? 4 : 3;
+}
+
 struct CacheShape {
-    int parts;          // chunks that the keys of all sequences are divided into, about
+    int parts;          // chunks that the keys of all sequences are divided into, about: what one round of blocks takes
     int min_tiles;      // a chunk has at least so many 32-key tiles
     int slots;          // chunks at most: one per sequence more than `parts`, or what the longest sequences could have
 };
-inline CacheShape cache_shape(int B, int Nq, int H, int Hkv, int64_t most)
+inline CacheShape cache_shape(int B, int Nq, int H, int Hkv, int d_qk, int bits, int64_t most)
 {
-    const int64_t rows = (int64_t)Nq * (H / Hkv), per = 16 * cache_row_blocks(Nq, H, Hkv);
-    const int64_t side = Hkv * ((rows + per - 1) / per);           // blocks per chunk
+    const int rb = cache_row_blocks(Nq, H, Hkv);
+    const int64_t rows = (int64_t)Nq * (H / Hkv);
+    const int64_t side = Hkv * ((rows + 16 * rb - 1) / (16 * rb)), round = 256 * cache_blocks_per_cu(d_qk, bits, rb);
     CacheShape s;
-    s.parts = (int)(side < 1024 ? 1024 / side : 1);
+    s.parts = (int)(side < round ? round / side : 1);
     s.min_tiles = 8;
     const int64_t tiles = (most + 31) / 32, each = (tiles + s.min_tiles - 1) / s.min_tiles;
     s.slots = (int)(B * each < (int64_t)s.parts + B ? B * (each ? each : 1) : s.parts + B);
@@ -65,7 +83,7 @@ struct RopeArgs {
     Stride3 sx[2], sdy[2], sy[2];
     const void* w[2];           // weights of the norms, or null: ones
     float* dw[2];               // their gradients, or null
-    float* part;                // partial sums of those: [blocks][2][d]
+    float* part;                // partial sums of those: [blocks of q, then of k][d]
     int heads[2];
     const float* freqs;
     const int* positions;       // or null: 0, 1, ... in every sequence
@@ -74,7 +92,7 @@ struct RopeArgs {
     float amplitude, sign, eps;
     bool interleaved, norm, backward, f16;
     void* stream;
-    int hg_shift, shares, units;     // rope_shape's (launch_rope sets them)
+    RopeShape shape[2];         // (launch_rope sets them)
 };
 int launch_rope(RopeArgs a);
 
