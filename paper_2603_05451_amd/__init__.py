@@ -112,7 +112,8 @@ def lib():
         address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
         _binding.bind(*(address(f) for f in (L.attn_fwd_dtype, L.attn_bwd_phases, L.attn_bwd_dtype, L.attn_bwd_workspace_bytes, L.attn_varlen_fwd_dtype,
                                              L.attn_varlen_bwd_dtype, L.attn_varlen_workspace_bytes, L.attn_fwd_strided, L.attn_bwd_strided,
-                                             L.attn_strided_workspace_bytes)),
+                                             L.attn_strided_workspace_bytes, L.attn_rope_fwd, L.attn_rope_bwd, L.attn_rope_workspace_bytes,
+                                             L.attn_cache_write, L.attn_cache_read, L.attn_cache_fwd, L.attn_cache_workspace_bytes)),
                       torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.nn.Parameter)
         _native = _binding
         _lib = L                # last: another thread that finds it set uses both
@@ -549,6 +550,9 @@ def attn_rope_fwd(q, k, freqs, positions=None, interleaved=False, offset=0, ampl
     (attn_rope_freqs): the rotated dims are offset ... offset + rot - 1, paired i with i + rot/2 or, interleaved, neighbours.
     positions: int32 [N], [B,N] ([T] for packed tokens), or None: 0 ... N-1.  -> (q_out, k_out), new contiguous tensors unless
     passed in; an output may be its input."""
+    r = (_native or _call()).rope_fwd(q, k, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, q_out, k_out, stream)
+    if r is not None:
+        return _done(r)
     x = _rows(q, "q", q.dtype, stream)
     code, dt = _dtype_code(q), q.dtype
     y = None if k is None else _rows(k, "k", dt, stream, (*q.shape[:-2], k.shape[-2], q.shape[-1]))
@@ -577,6 +581,10 @@ def attn_rope_bwd(dq, dk, freqs, positions=None, interleaved=False, offset=0, am
     """Backward of attn_rope_fwd: dq and dk are the gradients of its outputs (dk None where k was); q and k, its inputs, are needed
     with norms (eps) only.  -> (dq_in, dk_in, dq_weight, dk_weight): the gradients of q and k, and of the weights in fp32 [d]
     (None where there are no weights)."""
+    if dq_in is None and dk_in is None and workspace is None:
+        r = (_native or _call()).rope_bwd(dq, dk, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, q, k, stream)
+        if r is not None:
+            return _done(r)
     g = _rows(dq, "dq", dq.dtype, stream)
     code, dt = _dtype_code(dq), dq.dtype
     h = None if dk is None else _rows(dk, "dk", dt, stream, (*dq.shape[:-2], dk.shape[-2], dq.shape[-1]))
@@ -653,6 +661,9 @@ def _indexes(t, name, shape, stream):
 def attn_cache_write(k, v, slots, cache, stream=None):
     """Quantises k [T,Hkv,d_qk] and v [T,Hkv,d_v] (bf16 or fp16; views with a contiguous last axis) into slots int32 [T] of the cache
     (page * tokens-per-page + token in the page; negative or past the cache: the row is skipped; the others all different)."""
+    r = (_native or _call()).cache_write(k, v, slots, cache, stream)
+    if r is not None:
+        return _check(r)
     layout = _cache(cache, stream)
     code, dt, T = _dtype_code(k), k.dtype, k.shape[0]
     if k.dim() != 3 or v.dim() != 3:
@@ -666,6 +677,10 @@ def attn_cache_write(k, v, slots, cache, stream=None):
 def attn_cache_read(slots, cache, dtype, k=None, v=None, stream=None):
     """The rows at slots int32 [T] as bf16 or fp16 -> (k [T,Hkv,d_qk], v [T,Hkv,d_v]); zeros where a slot is negative or past the cache."""
     import torch
+    if k is None and v is None and (dtype is torch.bfloat16 or dtype is torch.float16):
+        r = (_native or _call()).cache_read(slots, cache, dtype is torch.float16, stream)
+        if r is not None:
+            return _done(r)
     layout = _cache(cache, stream)
     T = slots.shape[0] if slots.dim() == 1 else 0
     at = _indexes(slots, "slots", (T,), stream)
@@ -687,6 +702,9 @@ def attn_cache_fwd(q, cache, block_table, lens, scale, causal, o=None, lse=None,
     """Attention of q [B,Nq,H,d_qk] (a view with a contiguous last axis) over a paged cache: sequence b has lens[b] keys (int32 [B]), key j
     in page block_table[b, j // page] (int32 [B,width]); under the causal mask the last query sees the last key.
     -> (o [B,Nq,H,d_v], lse [B,H,Nq] fp32); a query without a visible key has o = 0 and lse = -inf."""
+    r = (_native or _call()).cache_fwd(q, cache, block_table, lens, scale, causal, o, lse, workspace, stream)
+    if r is not None:
+        return _done(r)
     import torch
     layout = _cache(cache, stream)
     code, dt = _dtype_code(q), q.dtype

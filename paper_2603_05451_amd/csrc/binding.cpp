@@ -25,6 +25,13 @@ decltype(&attn_varlen_workspace_bytes) p_varlen_bytes = nullptr;
 decltype(&attn_fwd_strided) p_fwd_strided = nullptr;
 decltype(&attn_bwd_strided) p_bwd_strided = nullptr;
 decltype(&attn_strided_workspace_bytes) p_strided_bytes = nullptr;
+decltype(&attn_rope_fwd) p_rope_fwd = nullptr;
+decltype(&attn_rope_bwd) p_rope_bwd = nullptr;
+decltype(&attn_rope_workspace_bytes) p_rope_bytes = nullptr;
+decltype(&attn_cache_write) p_cache_write = nullptr;
+decltype(&attn_cache_read) p_cache_read = nullptr;
+decltype(&attn_cache_fwd) p_cache_fwd = nullptr;
+decltype(&attn_cache_workspace_bytes) p_cache_bytes = nullptr;
 PyObject *get_device = nullptr, *get_stream = nullptr;      // torch._C._cuda_getDevice, _cuda_getCurrentRawStream
 PyTypeObject* parameter = nullptr;                          // torch.nn.Parameter
 
@@ -376,25 +383,325 @@ PyObject* bwd_strided(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// bind(ten addresses, in the order below; _cuda_getDevice, _cuda_getCurrentRawStream, Parameter)
+// ---- rotary positions and the quantised cache: calls on the current device's current stream (others are left to the Python text)
+
+// A call whose tensors all have to be on one device, the current one.
+struct CallHere : Call {
+    int64_t device = -1;
+    const at::Tensor* tensor(PyObject* x)
+    {
+        const at::Tensor* t = ok ? plain(x) : nullptr;
+        if (!t || !t->is_cuda() || (device >= 0 && t->device().index() != device)) { ok = false; return nullptr; }
+        device = t->device().index();
+        for (int64_t n : t->sizes()) fits(n);
+        return ok ? t : nullptr;
+    }
+    // [B, N, heads, d] or [T, heads, d] with a contiguous last axis; its strides are noted (0 along axes of one)
+    void* rows(const at::Tensor* t, at::ScalarType as, at::IntArrayRef shape = {})
+    {
+        const int64_t n = t ? t->dim() : 0;
+        if (!ok || (n != 3 && n != 4) || t->scalar_type() != as || (t->stride(n - 1) != 1 && t->size(n - 1) != 1) || (!shape.empty() && t->sizes() != shape)) {
+            ok = false;
+            return nullptr;
+        }
+        auto step = [&](int64_t i) -> long long { return i >= 0 && t->size(i) > 1 ? t->stride(i) : 0; };
+        strides[nstrides++] = {step(n - 4), step(n - 3), step(n - 2)};
+        return t->data_ptr();
+    }
+    void* none() { strides[nstrides++] = {0, 0, 0}; return nullptr; }
+    // contiguous, of this type and shape
+    void* flat(const at::Tensor* t, at::ScalarType as, at::IntArrayRef shape)
+    {
+        if (!ok || !t || t->scalar_type() != as || !t->is_contiguous() || t->sizes() != shape) { ok = false; return nullptr; }
+        return t->data_ptr();
+    }
+    int integer(PyObject* x)
+    {
+        const long n = PyLong_CheckExact(x) ? PyLong_AsLong(x) : -1;
+        if (PyErr_Occurred()) PyErr_Clear();
+        if (n < 0 || n > 0x7fffffff) ok = false;
+        return ok ? (int)n : 0;
+    }
+    void* stream_here(PyObject* x)
+    {
+        void* s = nullptr;
+        PyObject* d = x == Py_None && ok ? PyObject_CallNoArgs(get_device) : nullptr;
+        PyObject* h = d && PyLong_Check(d) && PyLong_AsLong(d) == device ? PyObject_CallOneArg(get_stream, d) : nullptr;
+        if (h && PyLong_Check(h)) s = PyLong_AsVoidPtr(h);
+        else ok = false;
+        if (PyErr_Occurred()) { PyErr_Clear(); ok = false; }
+        Py_XDECREF(h);
+        Py_XDECREF(d);
+        return s;
+    }
+    void element(const at::Tensor* t)
+    {
+        if (!t) return;
+        type = t->scalar_type();
+        if (type != at::kBFloat16 && type != at::kHalf) ok = false;
+        dtype = type == at::kHalf ? ATTN_F16 : ATTN_BF16;
+    }
+};
+
+// B, N, H, Hkv, d of rows q (and k, null: none), whose shapes have to agree
+struct RopeSizes {
+    int B, N, H, Hkv, d;
+    RopeSizes(CallHere& c, const at::Tensor* q, const at::Tensor* k)
+    {
+        const int64_t n = q ? q->dim() : 0;
+        if (!c.ok || (n != 3 && n != 4) || (k && k->dim() != n)) { c.ok = false; B = N = H = Hkv = d = 0; return; }
+        B = n == 4 ? size(q, 0) : 1;
+        N = size(q, (int)n - 3);
+        H = size(q, (int)n - 2);
+        d = size(q, (int)n - 1);
+        Hkv = k ? size(k, (int)n - 2) : 0;
+        for (int64_t i = 0; k && i < n; ++i)
+            if (i != n - 2 && k->size(i) != q->size(i)) c.ok = false;
+    }
+};
+
+// freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight at a[0] ... a[7]
+attn_rope_t rope_of(CallHere& c, PyObject* const* a, const RopeSizes& z, bool k)
+{
+    attn_rope_t r = {};
+    const at::Tensor* f = c.tensor(a[0]);
+    r.freqs = f && f->dim() == 1 ? (const float*)c.flat(f, at::kFloat, f->sizes()) : nullptr;
+    if (!r.freqs || f->size(0) > 4096) { c.ok = false; return r; }
+    r.rot = 2 * size(f, 0);
+    if (a[1] != Py_None) {
+        const at::Tensor* p = c.tensor(a[1]);
+        const bool each = p && p->dim() == 2;
+        const int64_t both[] = {z.B, z.N};
+        r.positions = (const int*)c.flat(p, at::kInt, each ? at::IntArrayRef(both, 2) : at::IntArrayRef(both + 1, 1));
+        r.positions_batch = each ? z.N : 0;
+    }
+    r.interleaved = c.truth(a[2]);
+    r.offset = c.integer(a[3]);
+    r.amplitude = (float)c.number(a[4]);
+    r.norm = a[5] != Py_None;
+    r.eps = r.norm ? (float)c.number(a[5]) : 0.f;
+    if (!r.norm && (a[6] != Py_None || a[7] != Py_None)) c.ok = false;
+    if (!k && a[7] != Py_None) c.ok = false;
+    const int64_t d = z.d;
+    if (a[6] != Py_None) r.q_weight = c.flat(c.tensor(a[6]), c.type, at::IntArrayRef(&d, 1));
+    if (a[7] != Py_None) r.k_weight = c.flat(c.tensor(a[7]), c.type, at::IntArrayRef(&d, 1));
+    return r;
+}
+
+// q, k, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, q_out, k_out, stream
+PyObject* rope_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    CallHere c;
+    if (n != 13) NOT_HERE;
+    const bool both = a[1] != Py_None;
+    const at::Tensor *q = c.tensor(a[0]), *k = both ? c.tensor(a[1]) : nullptr;
+    c.element(q);
+    const RopeSizes z(c, q, k);
+    if (!c.ok || (!both && a[11] != Py_None)) NOT_HERE;
+    const attn_rope_t r = rope_of(c, a + 2, z, both);
+    void *qp = c.rows(q, c.type), *kp = both ? c.rows(k, c.type) : c.none();
+    at::Tensor qo, ko;
+    if (a[10] != Py_None) { const at::Tensor* t = c.tensor(a[10]); if (t) qo = *t; }
+    if (a[11] != Py_None) { const at::Tensor* t = c.tensor(a[11]); if (t) ko = *t; }
+    if (!c.ok) NOT_HERE;
+    if (qo.defined() && qo.sizes() != q->sizes()) NOT_HERE;
+    if (ko.defined() && ko.sizes() != k->sizes()) NOT_HERE;
+    void* s = c.stream_here(a[12]);
+    if (!c.ok) NOT_HERE;
+    if (qo.defined() && (qo.scalar_type() != c.type || qo.stride(qo.dim() - 1) != 1)) NOT_HERE;
+    if (ko.defined() && (ko.scalar_type() != c.type || ko.stride(ko.dim() - 1) != 1)) NOT_HERE;
+    int rc;
+    {
+        Unlocked threads;
+        if (!qo.defined()) qo = at::empty(q->sizes(), q->options().requires_grad(false));
+        if (both && !ko.defined()) ko = at::empty(k->sizes(), k->options().requires_grad(false));
+        void *qop = c.rows(&qo, c.type), *kop = both ? c.rows(&ko, c.type) : c.none();
+        const attn_strides_t* st = c.strides;
+        rc = p_rope_fwd(c.dtype, &r, qp, st, kp, st + 1, qop, st + 2, kop, st + 3, z.B, z.N, z.H, z.Hkv, z.d, s);
+    }
+    if (rc != ATTN_OK) return PyLong_FromLong(rc);
+    if (!both) return Py_BuildValue("(NO)", out(a[10], qo), Py_None);
+    return outs(rc, {{a[10], &qo}, {a[11], &ko}});
+    END_HANDLE_TH_ERRORS
+}
+
+// dq, dk, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, q, k, stream (new outputs and workspace)
+PyObject* rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    CallHere c;
+    if (n != 13) NOT_HERE;
+    const bool both = a[1] != Py_None, norm = a[7] != Py_None;
+    const at::Tensor *g = c.tensor(a[0]), *h = both ? c.tensor(a[1]) : nullptr;
+    c.element(g);
+    const RopeSizes z(c, g, h);
+    if (!c.ok || (norm && (a[10] == Py_None || (a[11] != Py_None) != both))) NOT_HERE;
+    const attn_rope_t r = rope_of(c, a + 2, z, both);
+    const at::Tensor *q = norm ? c.tensor(a[10]) : nullptr, *k = norm && both ? c.tensor(a[11]) : nullptr;
+    void *gp = c.rows(g, c.type), *hp = both ? c.rows(h, c.type) : c.none();
+    void *qp = norm ? c.rows(q, c.type, c.ok ? g->sizes() : at::IntArrayRef()) : c.none(), *kp = norm && both ? c.rows(k, c.type, c.ok ? h->sizes() : at::IntArrayRef()) : c.none();
+    if (!c.ok) NOT_HERE;
+    const size_t need = r.q_weight || r.k_weight ? p_rope_bytes(z.B, z.N, z.H, z.Hkv, z.d) : 0;
+    void* s = c.stream_here(a[12]);
+    if (!c.ok) NOT_HERE;
+    at::Tensor gi, hi, wq, wk, ws;
+    int rc;
+    {
+        Unlocked threads;
+        const auto plain_options = g->options().requires_grad(false);
+        gi = at::empty(g->sizes(), plain_options);
+        if (both) hi = at::empty(h->sizes(), plain_options);
+        if (r.q_weight) wq = make_f32(*g, {z.d});
+        if (r.k_weight) wk = make_f32(*g, {z.d});
+        if (need || r.q_weight || r.k_weight) ws = make_bytes(*g, need);
+        void *gip = c.rows(&gi, c.type), *hip = both ? c.rows(&hi, c.type) : c.none();
+        const attn_strides_t* st = c.strides;
+        rc = p_rope_bwd(c.dtype, &r, gp, st, hp, st + 1, qp, st + 2, kp, st + 3, gip, st + 4, hip, st + 5, r.q_weight ? (float*)wq.data_ptr() : nullptr,
+                        r.k_weight ? (float*)wk.data_ptr() : nullptr, z.B, z.N, z.H, z.Hkv, z.d, ws.defined() ? ws.data_ptr() : nullptr,
+                        ws.defined() ? (size_t)ws.numel() : 0, s);
+    }
+    if (rc != ATTN_OK) return PyLong_FromLong(rc);
+    PyObject* t = PyTuple_New(4);
+    Py_ssize_t i = 0;
+    for (const at::Tensor* x : {&gi, &hi, &wq, &wk}) {
+        PyObject* o = x->defined() ? THPVariable_Wrap(*x) : (Py_INCREF(Py_None), Py_None);
+        PyTuple_SET_ITEM(t, i++, o);
+    }
+    return t;
+    END_HANDLE_TH_ERRORS
+}
+
+attn_cache_t cache_of(CallHere& c, PyObject* x)
+{
+    attn_cache_t r = {};
+    if (!PyTuple_Check(x) || PyTuple_GET_SIZE(x) != 4) { c.ok = false; return r; }
+    const at::Tensor* t[4];
+    void* p[4];
+    for (int i = 0; i < 4; ++i) {
+        t[i] = c.tensor(PyTuple_GET_ITEM(x, i));
+        if (!t[i] || t[i]->dim() != 4 || t[i]->scalar_type() != at::kByte || !t[i]->is_contiguous() || t[i]->sizes().slice(0, 3) != t[0]->sizes().slice(0, 3)) {
+            c.ok = false;
+            return r;
+        }
+        p[i] = t[i]->data_ptr();
+    }
+    const int64_t dk = 32 * t[1]->size(3), dv = 32 * t[3]->size(3), bits = t[0]->size(3) == dk ? 8 : 4;
+    if (dk > 4096 || dv > 4096 || t[0]->size(3) != dk * bits / 8 || t[2]->size(3) != dv * bits / 8) { c.ok = false; return r; }
+    return {p[0], p[1], p[2], p[3], size(t[0], 0), size(t[0], 2), size(t[0], 1), (int)dk, (int)dv, (int)bits};
+}
+
+// k, v, slots, cache, stream
+PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    CallHere c;
+    if (n != 5) NOT_HERE;
+    const at::Tensor *k = c.tensor(a[0]), *v = c.tensor(a[1]), *slots = c.tensor(a[2]);
+    c.element(k);
+    const attn_cache_t cache = cache_of(c, a[3]);
+    if (!c.ok || k->dim() != 3) NOT_HERE;
+    const int64_t T = k->size(0);
+    const int64_t ks[] = {T, cache.Hkv, cache.d_qk}, vs[] = {T, cache.Hkv, cache.d_v};
+    void *kp = c.rows(k, c.type, ks), *vp = c.rows(v, c.type, vs), *sp = c.flat(slots, at::kInt, at::IntArrayRef(&T, 1));
+    void* s = c.stream_here(a[4]);
+    if (!c.ok) NOT_HERE;
+    int rc;
+    {
+        Unlocked threads;
+        rc = p_cache_write(c.dtype, &cache, kp, c.strides, vp, c.strides + 1, (const int*)sp, (int)T, s);
+    }
+    return PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// slots, cache, whether fp16 (bf16 otherwise), stream (new outputs)
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    CallHere c;
+    if (n != 4) NOT_HERE;
+    const at::Tensor* slots = c.tensor(a[0]);
+    const attn_cache_t cache = cache_of(c, a[1]);
+    const int f16 = c.truth(a[2]);
+    if (!c.ok || slots->dim() != 1) NOT_HERE;
+    const int64_t T = slots->size(0);
+    void* sp = c.flat(slots, at::kInt, at::IntArrayRef(&T, 1));
+    void* s = c.stream_here(a[3]);
+    if (!c.ok) NOT_HERE;
+    at::Tensor k, v;
+    int rc;
+    {
+        Unlocked threads;
+        const auto options = slots->options().requires_grad(false).dtype(f16 ? at::kHalf : at::kBFloat16);
+        k = at::empty({T, cache.Hkv, cache.d_qk}, options);
+        v = at::empty({T, cache.Hkv, cache.d_v}, options);
+        rc = p_cache_read(f16 ? ATTN_F16 : ATTN_BF16, &cache, (const int*)sp, (int)T, k.data_ptr(), v.data_ptr(), s);
+    }
+    return outs(rc, {{Py_None, &k}, {Py_None, &v}});
+    END_HANDLE_TH_ERRORS
+}
+
+// q, cache, block_table, lens, scale, causal, o, lse, workspace, stream
+PyObject* cache_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    CallHere c;
+    if (n != 10) NOT_HERE;
+    const at::Tensor *q = c.tensor(a[0]), *table = c.tensor(a[2]), *lens = c.tensor(a[3]);
+    c.element(q);
+    const attn_cache_t cache = cache_of(c, a[1]);
+    if (!c.ok || q->dim() != 4 || table->dim() != 2) NOT_HERE;
+    const int B = size(q, 0), Nq = size(q, 1), H = size(q, 2), width = size(table, 1);
+    const double scale = c.number(a[4]);
+    const int causal = c.truth(a[5]);
+    const int64_t qs[] = {B, Nq, H, cache.d_qk}, os[] = {B, Nq, H, cache.d_v}, ts[] = {B, width}, ls[] = {B, H, Nq};
+    void *qp = c.rows(q, c.type, qs), *tp = c.flat(table, at::kInt, ts), *np = c.flat(lens, at::kInt, at::IntArrayRef(ts, 1));
+    at::Tensor o, lse, ws;
+    if (a[6] != Py_None) { const at::Tensor* t = c.tensor(a[6]); if (t) o = *t; }
+    if (a[7] != Py_None) { const at::Tensor* t = c.tensor(a[7]); c.flat(t, at::kFloat, ls); if (t) lse = *t; }
+    if (a[8] != Py_None) { const at::Tensor* t = c.tensor(a[8]); if (t) { ws = *t; if (ws.scalar_type() != at::kByte) c.ok = false; } }
+    if (o.defined()) { c.rows(&o, c.type, os); --c.nstrides; }
+    if (!c.ok) NOT_HERE;
+    const size_t need = ws.defined() ? 0 : p_cache_bytes(&cache, B, Nq, H, width);
+    void* s = c.stream_here(a[9]);
+    if (!c.ok) NOT_HERE;
+    int rc;
+    {
+        Unlocked threads;
+        if (!o.defined()) o = make(*q, {B, Nq, H, cache.d_v});
+        if (!lse.defined()) lse = make_f32(*q, {B, H, Nq});
+        if (!ws.defined()) ws = make_bytes(*q, need);
+        void* op = c.rows(&o, c.type, os);
+        rc = p_cache_fwd(c.dtype, &cache, qp, c.strides, op, c.strides + 1, (float*)lse.data_ptr(), (const int*)tp, width, (const int*)np, B, Nq, H, (float)scale,
+                         causal, ws.data_ptr(), (size_t)ws.numel(), s);
+    }
+    return outs(rc, {{a[6], &o}, {a[7], &lse}});
+    END_HANDLE_TH_ERRORS
+}
+
+// bind(the addresses, in the order below; _cuda_getDevice, _cuda_getCurrentRawStream, Parameter)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     void** const to[] = {(void**)&p_fwd, (void**)&p_bwd_phases, (void**)&p_bwd_dtype, (void**)&p_bwd_bytes, (void**)&p_varlen_fwd, (void**)&p_varlen_bwd,
-                         (void**)&p_varlen_bytes, (void**)&p_fwd_strided, (void**)&p_bwd_strided, (void**)&p_strided_bytes};
-    if (n != 13 || !PyType_Check(a[12])) { PyErr_SetString(PyExc_TypeError, "bind: ten addresses, two functions, a type"); return nullptr; }
-    for (int i = 0; i < 10; ++i) {
+                         (void**)&p_varlen_bytes, (void**)&p_fwd_strided, (void**)&p_bwd_strided, (void**)&p_strided_bytes, (void**)&p_rope_fwd, (void**)&p_rope_bwd,
+                         (void**)&p_rope_bytes, (void**)&p_cache_write, (void**)&p_cache_read, (void**)&p_cache_fwd, (void**)&p_cache_bytes};
+    constexpr int N = sizeof(to) / sizeof(to[0]);
+    if (n != N + 3 || !PyType_Check(a[N + 2])) { PyErr_SetString(PyExc_TypeError, "bind: the addresses, two functions, a type"); return nullptr; }
+    for (int i = 0; i < N; ++i) {
         *to[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred()) return nullptr;
     }
-    for (int i = 10; i < 13; ++i) Py_INCREF(a[i]);
-    get_device = a[10];
-    get_stream = a[11];
-    parameter = (PyTypeObject*)a[12];
+    for (int i = N; i < N + 3; ++i) Py_INCREF(a[i]);
+    get_device = a[N];
+    get_stream = a[N + 1];
+    parameter = (PyTypeObject*)a[N + 2];
     Py_RETURN_NONE;
 }
 
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(fwd), METHOD(bwd), METHOD(varlen_fwd), METHOD(varlen_bwd), METHOD(fwd_strided), METHOD(bwd_strided),
+                         METHOD(rope_fwd), METHOD(rope_bwd), METHOD(cache_write), METHOD(cache_read), METHOD(cache_fwd),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
