@@ -49,75 +49,121 @@ __device__ __forceinline__ int wave_prefix(int x)
 }
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
 
-// Keys of sequence b as the kernels take them: no more than its row of the table has room for, none if the length is negative.
-__device__ __forceinline__ int cache_length(const CachePlanArgs& p, const int* __restrict__ lens, int b)
-{
-    return b < p.B ? min(max(lens[b], 0), p.most) : 0;
-}
-// Tiles of a chunk: all keys in about `parts` chunks, whole turns of the four waves, not below min_tiles.
-__device__ __forceinline__ int cache_chunk_tiles(const CachePlanArgs& p, const int* __restrict__ lens)
-{
-    int total = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) total += (cache_length(p, lens, b0 + (threadIdx.x & 63)) + 31) >> 5;
-    total = wave_sum(total);
-    return max(((total + p.parts - 1) / p.parts + 3) & ~3, p.min_tiles);
-}
-// The chunks of a sequence: whole ones, and one that is shorter (also if there are no keys, for its rows have results).
+// The chunks of a sequence: whole ones, and one that is shorter (also if there are no keys, for its rows have results), which is of class
+// 1 ... 4 by its length in quarters, the longest first.
 struct CacheSplit {
-    int whole, rest;
+    int whole, rest;            // rest: its class, 0 if there is none
 };
-__device__ __forceinline__ CacheSplit cache_split(int len, int chunk_tiles)
-{
-    const int tiles = (len + 31) >> 5, whole = tiles / chunk_tiles;
-    return {whole, tiles > whole * chunk_tiles || tiles == 0};
-}
 
-// The sequence and chunk at place `slot` of all chunks: the whole ones of all sequences, in order, then the shorter ones, so that
-// these fill up what the others leave.  False behind the last one.
+// What every wave of a launch finds out from the lengths, a sequence per lane; those of the first 512 sequences are loaded at once and
+// stay in registers (300 sequences of 500 keys, 8 heads, d = 128: 58 us with the loads of 64 sequences one after the other, three times).
+struct CacheLengths {
+    static constexpr int HELD = 8;
+    const CachePlanArgs& p;
+    const int* __restrict__ lens;
+    int held[HELD], chunk_tiles;
+
+    // Keys of sequence b as the kernels take them: no more than its row of the table has room for, none if the length is negative.
+    __device__ __forceinline__ int fetch(int b) const { return b < p.B ? min(max(lens[b], 0), p.most) : 0; }
+    // f(first of 64 sequences, length of the lane's), in order, until it says true
+    template <typename F>
+    __device__ __forceinline__ void each(F&& f) const
+    {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (64 * i >= p.B || f(64 * i, held[i])) return;
+        for (int b0 = 64 * HELD; b0 < p.B; b0 += 64)
+            if (f(b0, fetch(b0 + (threadIdx.x & 63)))) return;
+    }
+    __device__ __forceinline__ CacheLengths(const CachePlanArgs& plan, const int* __restrict__ l) : p(plan), lens(l)
+    {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) held[i] = 64 * i < p.B ? fetch(64 * i + (threadIdx.x & 63)) : 0;
+        // tiles of a chunk: all keys in about `parts` chunks, whole turns of the four waves, not below min_tiles
+        int total = 0;
+        each([&](int, int len) { total += (len + 31) >> 5; return false; });
+        total = wave_sum(total);
+        chunk_tiles = max(((total + p.parts - 1) / p.parts + 3) & ~3, p.min_tiles);
+    }
+    __device__ __forceinline__ CacheSplit split(int b, int len) const
+    {
+        if (b >= p.B) return {0, 0};
+        const int tiles = (len + 31) >> 5, whole = tiles / chunk_tiles, r = 4 * (tiles - whole * chunk_tiles);
+        return {whole, r == 0 && tiles > 0 ? 0 : 4 - (r >= chunk_tiles) - (r >= 2 * chunk_tiles) - (r >= 3 * chunk_tiles)};
+    }
+    // chunks of the five kinds: n[0] whole ones, n[1 ... 4] shorter ones
+    __device__ __forceinline__ void count(int (&n)[5]) const
+    {
+#pragma unroll
+        for (int c = 0; c < 5; ++c) n[c] = 0;
+        each([&](int b0, int len) {
+            const CacheSplit s = split(b0 + (threadIdx.x & 63), len);
+            n[0] += s.whole;
+#pragma unroll
+            for (int c = 1; c < 5; ++c) n[c] += s.rest == c;
+            return false;
+        });
+#pragma unroll
+        for (int c = 0; c < 5; ++c) n[c] = wave_sum(n[c]);
+    }
+};
+
+// The sequence and chunk at place `slot` of all chunks: kind by kind, in the sequences' order within a kind.  The longest first, so that the
+// shorter ones fill up what the others leave (48 sequences of 67 ... 7696 keys, 8 heads, d = 128, 4 bits: 24.8 us with the shorter chunks in
+// the sequences' order, 21.5 so; 19.5 where all have the mean length).  False behind the last chunk.
 __device__ __forceinline__ bool cache_place(const CachePlanArgs& p, const int* __restrict__ lens, int slot, CachePlace& at)
 {
-    at.chunk_tiles = cache_chunk_tiles(p, lens);
-    for (int pass = 0; pass < 2; ++pass)
-        for (int b0 = 0; b0 < p.B; b0 += 64) {
-            const int b = b0 + (threadIdx.x & 63);
-            const int len = cache_length(p, lens, b);
-            const CacheSplit split = b < p.B ? cache_split(len, at.chunk_tiles) : CacheSplit{0, 0};
-            const int n = pass ? split.rest : split.whole;
-            const int upto = wave_prefix(n);
-            const uint64_t past = __ballot(upto > slot);
-            if (past) {
-                const int l = __builtin_ctzll(past);
-                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-                at.b = b0 + l;
-                at.len = of(len);
-                at.chunks = of(split.whole + split.rest);
-                at.chunk = pass ? of(split.whole) : slot - (of(upto) - of(n));
-                return true;
-            }
-            slot -= __builtin_amdgcn_readlane(upto, 63);
+    const CacheLengths all(p, lens);
+    at.chunk_tiles = all.chunk_tiles;
+    int n[5], kind = 0;
+    all.count(n);
+#pragma unroll
+    for (int c = 0; c < 5; ++c)
+        if (kind == c && slot >= n[c]) { slot -= n[c]; kind = c + 1; }
+    if (kind == 5) return false;
+    all.each([&](int b0, int len) {
+        const CacheSplit split = all.split(b0 + (threadIdx.x & 63), len);
+        const int mine = kind ? split.rest == kind : split.whole;
+        const int upto = wave_prefix(mine);
+        const uint64_t past = __ballot(upto > slot);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+            at.b = b0 + l;
+            at.len = of(len);
+            at.chunks = of(split.whole + (split.rest > 0));
+            at.chunk = kind ? of(split.whole) : slot - (of(upto) - of(mine));
+            return true;
         }
-    return false;
+        slot -= __builtin_amdgcn_readlane(upto, 63);
+        return false;
+    });
+    return true;
 }
-// The places of sequence b's first whole chunk and of its shorter one (if there is one).
-__device__ __forceinline__ void cache_place_of(const CachePlanArgs& p, const int* __restrict__ lens, int b, CachePlace& at, int& slot0, int& rest)
+// The chunks of sequence b, and, if there are more than one, the places of its first whole one and of its shorter one (-1: there is none).
+__device__ __forceinline__ int cache_places_of(const CachePlanArgs& p, const int* __restrict__ lens, int b, int& slot0, int& rest)
 {
-    at.b = b;
-    at.chunk_tiles = cache_chunk_tiles(p, lens);
-    at.chunk = 0;
-    int whole = 0, before = 0, rests = 0, len = 0;      // whole chunks of all, those before b, shorter ones before b
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
+    const CacheLengths all(p, lens);
+    const CacheSplit mine = all.split(b, all.fetch(b));
+    const int chunks = mine.whole + (mine.rest > 0);
+    if (chunks == 1) return 1;
+    int n[5], before = 0, same = 0;                         // whole chunks and shorter ones of the same kind of the sequences before b
+    all.count(n);
+    all.each([&](int b0, int len) {
         const int i = b0 + (threadIdx.x & 63);
-        const int n = cache_length(p, lens, i);
-        const CacheSplit split = i < p.B ? cache_split(n, at.chunk_tiles) : CacheSplit{0, 0};
-        whole += split.whole;
-        if (i < b) { before += split.whole; rests += split.rest; }
-        if (i == b) len = n;
-    }
-    at.len = wave_sum(len);
-    const CacheSplit mine = cache_split(at.len, at.chunk_tiles);
-    at.chunks = mine.whole + mine.rest;
+        const CacheSplit split = all.split(i, len);
+        if (i < b) { before += split.whole; same += split.rest == mine.rest; }
+        return false;
+    });
     slot0 = wave_sum(before);
-    rest = mine.rest ? wave_sum(whole) + wave_sum(rests) : -1;
+    rest = -1;
+    if (mine.rest) {
+        rest = wave_sum(same);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (c < mine.rest) rest += n[c];
+    }
+    return chunks;
 }
 
 #if ATTN_F16

@@ -69,6 +69,10 @@ inline CacheShape cache_shape(int B, int Nq, int H, int Hkv, int d_qk, int bits,
     return s;
 }
 
+// Rows (query, head) that a block of the merge takes: more where there are more than the chip's blocks, for each finds its sequence's
+// chunks first.
+inline int cache_merge_rows(int64_t rows) { return rows < 1024 ? 1 : rows < 16 * 1024 ? (int)(rows / 1024) : 16; }
+
 }  // namespace attn
 
 #if defined(__HIP__)
