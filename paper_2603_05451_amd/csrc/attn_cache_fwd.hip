@@ -28,7 +28,7 @@ __device__ __forceinline__ float xquarter_sum(float x)
 // ---- which keys a block takes, from the lengths in device memory
 struct CachePlanArgs {
     int B, Hkv, page_shift, most;       // most: keys that a row of the table has room for
-    int parts, min_tiles;               // cache_shape's
+    int parts, min_tiles, waves;        // cache_shape's
 };
 struct CachePlace {
     int b, len, chunk, chunks, chunk_tiles;     // of a sequence; chunks of chunk_tiles 32-key tiles
@@ -62,6 +62,7 @@ struct CacheLengths {
     const CachePlanArgs& p;
     const int* __restrict__ lens;
     int held[HELD], chunk_tiles;
+    float per_chunk;
 
     // Keys of sequence b as the kernels take them: no more than its row of the table has room for, none if the length is negative.
     __device__ __forceinline__ int fetch(int b) const { return b < p.B ? min(max(lens[b], 0), p.most) : 0; }
@@ -79,16 +80,24 @@ struct CacheLengths {
     {
 #pragma unroll
         for (int i = 0; i < HELD; ++i) held[i] = 64 * i < p.B ? fetch(64 * i + (threadIdx.x & 63)) : 0;
-        // tiles of a chunk: all keys in about `parts` chunks, whole turns of the four waves, not below min_tiles
-        int total = 0;
-        each([&](int, int len) { total += (len + 31) >> 5; return false; });
+        // tiles of a chunk: all keys in about `parts` chunks, but the mean sequence in equal ones (of 1.2 chunks it would leave most of a
+        // block's or wave's time unused); whole turns of its waves, not below min_tiles
+        int total = 0, used = 0;
+        each([&](int, int len) { total += (len + 31) >> 5; used += len > 0; return false; });
         total = wave_sum(total);
-        chunk_tiles = max(((total + p.parts - 1) / p.parts + 3) & ~3, p.min_tiles);
+        const uint32_t even = (uint32_t)(total + p.parts - 1) / p.parts, mean = (uint32_t)total / max(wave_sum(used), 1);
+        const uint32_t n = (4 * mean + even) / max(4 * even, 1u);                      // mean / even, less a quarter, rounded
+        chunk_tiles = max(((int)(n ? (mean + n - 1) / n : even) + p.waves - 1) & -p.waves, p.min_tiles);
+        per_chunk = 1.0f / (float)chunk_tiles;
     }
     __device__ __forceinline__ CacheSplit split(int b, int len) const
     {
         if (b >= p.B) return {0, 0};
-        const int tiles = (len + 31) >> 5, whole = tiles / chunk_tiles, r = 4 * (tiles - whole * chunk_tiles);
+        const int tiles = (len + 31) >> 5;
+        int whole = (int)((float)tiles * per_chunk), r = tiles - whole * chunk_tiles;      // (up to 2^26 / 8: off by one at most)
+        if (r < 0) { --whole; r += chunk_tiles; }
+        if (r >= chunk_tiles) { ++whole; r -= chunk_tiles; }
+        r *= 4;
         return {whole, r == 0 && tiles > 0 ? 0 : 4 - (r >= chunk_tiles) - (r >= 2 * chunk_tiles) - (r >= 3 * chunk_tiles)};
     }
     // chunks of the five kinds: n[0] whole ones, n[1 ... 4] shorter ones

@@ -52,20 +52,26 @@ constexpr int cache_blocks_per_cu(int d_qk, int bits, int row_blocks)
 }
 
 struct CacheShape {
+    int waves;          // that share a chunk: the four of a block, or one
     int parts;          // chunks that the keys of all sequences are divided into, about: what one round of blocks takes
     int min_tiles;      // a chunk has at least so many 32-key tiles
-    int slots;          // chunks at most: one per sequence more than `parts`, or what the longest sequences could have
+    int slots;          // chunks at most: `parts` of three quarters of that length and one per sequence, or what the longest could have
 };
+// Where there are more (sequence, KV head, row group)s than the chip holds blocks, each is a wave's work: a block per one of them would take
+// several rounds, whose first loads and merges (5 us each) all blocks go through at the same time.
 inline CacheShape cache_shape(int B, int Nq, int H, int Hkv, int d_qk, int bits, int64_t most)
 {
     const int rb = cache_row_blocks(Nq, H, Hkv);
     const int64_t rows = (int64_t)Nq * (H / Hkv);
     const int64_t side = Hkv * ((rows + 16 * rb - 1) / (16 * rb)), round = 256 * cache_blocks_per_cu(d_qk, bits, rb);
     CacheShape s;
-    s.parts = (int)(side < round ? round / side : 1);
+    s.waves = B * side >= round ? 1 : 4;
+    const int64_t places = round * (4 / s.waves);
+    s.parts = (int)(side < places ? places / side : 1);
     s.min_tiles = 8;
     const int64_t tiles = (most + 31) / 32, each = (tiles + s.min_tiles - 1) / s.min_tiles;
-    s.slots = (int)(B * each < (int64_t)s.parts + B ? B * (each ? each : 1) : s.parts + B);
+    const int64_t most_parts = ((int64_t)s.parts * 4 + 2) / 3 + B;
+    s.slots = (int)(B * each < most_parts ? B * each : most_parts);
     return s;
 }
 

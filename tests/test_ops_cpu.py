@@ -189,7 +189,7 @@ extern "C" {
 void t_cache(int B, int Nq, int H, int Hkv, int d, int bits, long long most, int* out)
 {
     const CacheShape s = cache_shape(B, Nq, H, Hkv, d, bits, most);
-    out[0] = s.parts; out[1] = s.min_tiles; out[2] = s.slots; out[3] = cache_row_blocks(Nq, H, Hkv);
+    out[0] = s.parts; out[1] = s.min_tiles; out[2] = s.slots; out[3] = cache_row_blocks(Nq, H, Hkv); out[4] = s.waves;
 }
 void t_rope(int tokens, int heads, int d, int sums, int* out)
 {
@@ -209,7 +209,7 @@ def rules(tmp_path_factory):
     lib.t_cache.argtypes = [ctypes.c_int] * 6 + [ctypes.c_longlong, ctypes.c_void_p]
 
     def call(name, *a):
-        out = (ctypes.c_int * 4)()
+        out = (ctypes.c_int * 5)()
         getattr(lib, name)(*a, out)
         return list(out)
     return call
@@ -223,11 +223,13 @@ def test_chunks_fit_the_launch(rules):
         H, page = Hkv * r.choice([1, 3, 8]), 1 << r.randint(4, 8)
         width = int(2 ** r.uniform(0, 10))
         most = width * page
-        parts, min_tiles, slots, wide = rules("t_cache", B, Nq, H, Hkv, r.choice([64, 96, 128, 192, 256]), r.choice([4, 8]), most)
-        assert parts >= 1 and min_tiles % 4 == 0 and slots >= B and wide == (2 if Nq * H // Hkv > 16 else 1)
+        parts, min_tiles, slots, wide, waves = rules("t_cache", B, Nq, H, Hkv, r.choice([64, 96, 128, 192, 256]), r.choice([4, 8]), most)
+        assert parts >= 1 and min_tiles % 4 == 0 and waves in (1, 4) and slots >= B and wide == (2 if Nq * H // Hkv > 16 else 1)
         for lens in ([most] * B, [0] * B, [r.randint(0, most) for _ in range(B)], [most] + [1] * (B - 1)):
             tiles = [(n + 31) // 32 for n in lens]
-            chunk = max((-(-sum(tiles) // parts) + 3) // 4 * 4, min_tiles)
+            even, mean = -(-sum(tiles) // parts), sum(tiles) // max(sum(t > 0 for t in tiles), 1)
+            n = (4 * mean + even) // max(4 * even, 1)
+            chunk = max(((-(-mean // n) if n else even) + waves - 1) // waves * waves, min_tiles)
             used = sum(max(1, -(-t // chunk)) for t in tiles)
             assert used <= slots, (B, Nq, H, Hkv, most, lens[:5])
             if slots == B:
@@ -239,7 +241,7 @@ def test_rows_of_rotary_calls_are_all_taken(rules):
     r = random.Random(2)
     for _ in range(300):
         tokens, heads, d, sums = int(2 ** r.uniform(0, 12)), r.randint(1, 80), r.choice([64, 96, 128, 192, 256]), r.randint(0, 1)
-        blocks, shift, shares, lanes = rules("t_rope", tokens, heads, d, sums)
+        blocks, shift, shares, lanes, _ = rules("t_rope", tokens, heads, d, sums)
         assert lanes * 16 >= d and blocks % shares == 0 and blocks > 0
         if sums:
             assert blocks <= 512 + shares
