@@ -581,10 +581,10 @@ def attn_rope_bwd(dq, dk, freqs, positions=None, interleaved=False, offset=0, am
     """Backward of attn_rope_fwd: dq and dk are the gradients of its outputs (dk None where k was); q and k, its inputs, are needed
     with norms (eps) only.  -> (dq_in, dk_in, dq_weight, dk_weight): the gradients of q and k, and of the weights in fp32 [d]
     (None where there are no weights)."""
-    if dq_in is None and dk_in is None and workspace is None:
-        r = (_native or _call()).rope_bwd(dq, dk, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, q, k, stream)
-        if r is not None:
-            return _done(r)
+    r = (_native or _call()).rope_bwd(dq, dk, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, q, k, dq_in, dk_in,
+                                      workspace, stream)
+    if r is not None:
+        return _done(r)
     g = _rows(dq, "dq", dq.dtype, stream)
     code, dt = _dtype_code(dq), dq.dtype
     h = None if dk is None else _rows(dk, "dk", dt, stream, (*dq.shape[:-2], dk.shape[-2], dq.shape[-1]))
@@ -677,8 +677,8 @@ def attn_cache_write(k, v, slots, cache, stream=None):
 def attn_cache_read(slots, cache, dtype, k=None, v=None, stream=None):
     """The rows at slots int32 [T] as bf16 or fp16 -> (k [T,Hkv,d_qk], v [T,Hkv,d_v]); zeros where a slot is negative or past the cache."""
     import torch
-    if k is None and v is None and (dtype is torch.bfloat16 or dtype is torch.float16):
-        r = (_native or _call()).cache_read(slots, cache, dtype is torch.float16, stream)
+    if dtype is torch.bfloat16 or dtype is torch.float16:
+        r = (_native or _call()).cache_read(slots, cache, dtype is torch.float16, k, v, stream)
         if r is not None:
             return _done(r)
     layout = _cache(cache, stream)

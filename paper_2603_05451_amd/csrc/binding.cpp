@@ -526,35 +526,40 @@ PyObject* rope_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// dq, dk, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, q, k, stream (new outputs and workspace)
+// dq, dk, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, q, k, dq_in, dk_in, workspace, stream
 PyObject* rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     CallHere c;
-    if (n != 13) NOT_HERE;
+    if (n != 16) NOT_HERE;
     const bool both = a[1] != Py_None, norm = a[7] != Py_None;
     const at::Tensor *g = c.tensor(a[0]), *h = both ? c.tensor(a[1]) : nullptr;
     c.element(g);
     const RopeSizes z(c, g, h);
-    if (!c.ok || (norm && (a[10] == Py_None || (a[11] != Py_None) != both))) NOT_HERE;
+    if (!c.ok || (norm && (a[10] == Py_None || (a[11] != Py_None) != both)) || (!both && a[13] != Py_None)) NOT_HERE;
     const attn_rope_t r = rope_of(c, a + 2, z, both);
     const at::Tensor *q = norm ? c.tensor(a[10]) : nullptr, *k = norm && both ? c.tensor(a[11]) : nullptr;
+    const at::IntArrayRef gs = g->sizes(), hs = both ? h->sizes() : at::IntArrayRef();
     void *gp = c.rows(g, c.type), *hp = both ? c.rows(h, c.type) : c.none();
-    void *qp = norm ? c.rows(q, c.type, c.ok ? g->sizes() : at::IntArrayRef()) : c.none(), *kp = norm && both ? c.rows(k, c.type, c.ok ? h->sizes() : at::IntArrayRef()) : c.none();
-    if (!c.ok) NOT_HERE;
-    const size_t need = r.q_weight || r.k_weight ? p_rope_bytes(z.B, z.N, z.H, z.Hkv, z.d) : 0;
-    void* s = c.stream_here(a[12]);
-    if (!c.ok) NOT_HERE;
+    void *qp = norm ? c.rows(q, c.type, gs) : c.none(), *kp = norm && both ? c.rows(k, c.type, hs) : c.none();
     at::Tensor gi, hi, wq, wk, ws;
+    if (a[12] != Py_None) { const at::Tensor* t = c.tensor(a[12]); if (t) { gi = *t; c.rows(t, c.type, gs); --c.nstrides; } }
+    if (a[13] != Py_None) { const at::Tensor* t = c.tensor(a[13]); if (t) { hi = *t; c.rows(t, c.type, hs); --c.nstrides; } }
+    if (a[14] != Py_None) { const at::Tensor* t = c.tensor(a[14]); if (t) { ws = *t; if (t->scalar_type() != at::kByte) c.ok = false; } }
+    if (!c.ok) NOT_HERE;
+    const bool sums = r.q_weight || r.k_weight;
+    const size_t need = sums && !ws.defined() ? p_rope_bytes(z.B, z.N, z.H, z.Hkv, z.d) : 0;
+    void* s = c.stream_here(a[15]);
+    if (!c.ok) NOT_HERE;
     int rc;
     {
         Unlocked threads;
-        const auto plain_options = g->options().requires_grad(false);
-        gi = at::empty(g->sizes(), plain_options);
-        if (both) hi = at::empty(h->sizes(), plain_options);
+        const auto options = g->options().requires_grad(false);
+        if (!gi.defined()) gi = at::empty(gs, options);
+        if (both && !hi.defined()) hi = at::empty(hs, options);
         if (r.q_weight) wq = make_f32(*g, {z.d});
         if (r.k_weight) wk = make_f32(*g, {z.d});
-        if (need || r.q_weight || r.k_weight) ws = make_bytes(*g, need);
+        if (sums && !ws.defined()) ws = make_bytes(*g, need);
         void *gip = c.rows(&gi, c.type), *hip = both ? c.rows(&hi, c.type) : c.none();
         const attn_strides_t* st = c.strides;
         rc = p_rope_bwd(c.dtype, &r, gp, st, hp, st + 1, qp, st + 2, kp, st + 3, gip, st + 4, hip, st + 5, r.q_weight ? (float*)wq.data_ptr() : nullptr,
@@ -563,10 +568,12 @@ PyObject* rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     }
     if (rc != ATTN_OK) return PyLong_FromLong(rc);
     PyObject* t = PyTuple_New(4);
-    Py_ssize_t i = 0;
-    for (const at::Tensor* x : {&gi, &hi, &wq, &wk}) {
-        PyObject* o = x->defined() ? THPVariable_Wrap(*x) : (Py_INCREF(Py_None), Py_None);
-        PyTuple_SET_ITEM(t, i++, o);
+    PyObject* const mine[] = {a[12], a[13], Py_None, Py_None};
+    const at::Tensor* const made[] = {&gi, &hi, &wq, &wk};
+    for (Py_ssize_t i = 0; i < 4; ++i) {
+        PyObject* x = made[i]->defined() ? out(mine[i], *made[i]) : Py_None;
+        if (x == Py_None) Py_INCREF(x);
+        PyTuple_SET_ITEM(t, i, x);
     }
     return t;
     END_HANDLE_TH_ERRORS
@@ -615,30 +622,34 @@ PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// slots, cache, whether fp16 (bf16 otherwise), stream (new outputs)
+// slots, cache, whether fp16 (bf16 otherwise), k, v, stream
 PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     CallHere c;
-    if (n != 4) NOT_HERE;
+    if (n != 6) NOT_HERE;
     const at::Tensor* slots = c.tensor(a[0]);
     const attn_cache_t cache = cache_of(c, a[1]);
     const int f16 = c.truth(a[2]);
     if (!c.ok || slots->dim() != 1) NOT_HERE;
     const int64_t T = slots->size(0);
     void* sp = c.flat(slots, at::kInt, at::IntArrayRef(&T, 1));
-    void* s = c.stream_here(a[3]);
-    if (!c.ok) NOT_HERE;
+    const auto as = f16 ? at::kHalf : at::kBFloat16;
+    const int64_t ks[] = {T, cache.Hkv, cache.d_qk}, vs[] = {T, cache.Hkv, cache.d_v};
     at::Tensor k, v;
+    if (a[3] != Py_None) { const at::Tensor* t = c.tensor(a[3]); c.flat(t, as, ks); if (t) k = *t; }
+    if (a[4] != Py_None) { const at::Tensor* t = c.tensor(a[4]); c.flat(t, as, vs); if (t) v = *t; }
+    void* s = c.stream_here(a[5]);
+    if (!c.ok) NOT_HERE;
     int rc;
     {
         Unlocked threads;
-        const auto options = slots->options().requires_grad(false).dtype(f16 ? at::kHalf : at::kBFloat16);
-        k = at::empty({T, cache.Hkv, cache.d_qk}, options);
-        v = at::empty({T, cache.Hkv, cache.d_v}, options);
+        const auto options = slots->options().requires_grad(false).dtype(as);
+        if (!k.defined()) k = at::empty(ks, options);
+        if (!v.defined()) v = at::empty(vs, options);
         rc = p_cache_read(f16 ? ATTN_F16 : ATTN_BF16, &cache, (const int*)sp, (int)T, k.data_ptr(), v.data_ptr(), s);
     }
-    return outs(rc, {{Py_None, &k}, {Py_None, &v}});
+    return outs(rc, {{a[3], &k}, {a[4], &v}});
     END_HANDLE_TH_ERRORS
 }
 
