@@ -328,8 +328,10 @@ int attn_cache_read(int dtype, const attn_cache_t* cache, const int* slots, int 
  *     lse = -inf.  A negative length counts as 0, one beyond table_width * page as that.
  *   - Entries of the table behind a sequence's last key are not read.  A page number outside the cache makes the rows that see
  *     its keys NaN; nothing outside the tensors is touched.
- *   - A key or value that is NaN reaches the queries that see it and no others; what the slots behind the last key hold (never
- *     written, another sequence's, NaN) reaches none.
+ *   - A block of a key or value that is NaN (scale byte 255) reaches the queries that see it and no others; what the slots behind
+ *     the last key hold (never written, another sequence's, NaN) reaches none.  (e4m3's own NaN, 0x7f, which attn_cache_write does
+ *     not write, may reach earlier queries of the call.)  For fp16 queries the cache's numbers are taken as fp16: infinite beyond
+ *     its range.
  *   - Lengths and pages are read on the device: a captured call may be replayed with others.  Any Nq works; it is meant for few
  *     (one token, a few drafted ones): a long chunk reads its keys back (attn_cache_read) for attn_varlen_fwd.
  *   workspace: attn_cache_workspace_bytes(...) bytes, 256-byte aligned, contents ignored.  One kernel, and a merge where the table

@@ -476,9 +476,10 @@ def _here(t, name, dtype, stream):
     import torch
     if not (t.is_cuda and t.dtype == dtype):
         raise ValueError(f"{name} must be a {dtype} CUDA tensor")
-    device = stream.device.index if stream is not None else torch.cuda.current_device()
-    if t.device.index != device:
-        raise ValueError(f"{name} is on {t.device}, the call runs on device {device}: make its device the current one")
+    device = torch.cuda.current_device()
+    if t.device.index != device or (stream is not None and stream.device.index != device):
+        raise ValueError(f"{name} is on {t.device}, the stream on {t.device if stream is None else stream.device}, the current device is {device}: "
+                         "a call's tensors and stream belong to the current device")
 
 
 def _rows(t, name, dtype, stream, shape=None):

@@ -49,7 +49,7 @@ inline int cache_row_blocks(int Nq, int H, int Hkv) { return (int64_t)Nq * (H / 
 // Blocks of the attention kernel that a CU holds: what its registers allow (the kernel is compiled for it).
 constexpr int cache_blocks_per_cu(int d_qk, int bits, int row_blocks)
 {
-    return d_qk > 192 ? 1 : d_qk > 128 ? (bits == 8 && row_blocks == 2 ? 1 : 2) : d_qk > 64 ? (bits == 4 && row_blocks == 1 ? 3 : 2) : row_blocks == 1 ? 4 : 3;
+    return d_qk > 192 ? (bits == 4 && row_blocks == 1 ? 2 : 1) : d_qk > 128 ? (bits == 8 && row_blocks == 2 ? 1 : 2) : d_qk > 64 ? (bits == 4 && row_blocks == 1 ? 3 : 2) : row_blocks == 1 ? 4 : 3;
 }
 
 struct CacheShape {

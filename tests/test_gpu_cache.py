@@ -203,6 +203,37 @@ def test_divided_keys(dtype, lens, H, Hkv, bits):
     _run(4, lens, 1, H, Hkv, 64, 64, bits, 64, dtype, True)
 
 
+@pytest.mark.parametrize("dqk,dv,bits,B,Nq,H,Hkv,dtype", [
+    (64, 64, 4, 600, 1, 4, 2, BF), (64, 64, 8, 530, 3, 12, 2, HF), (96, 96, 4, 400, 1, 2, 2, HF), (96, 96, 8, 270, 5, 8, 2, BF), (128, 128, 4, 400, 1, 2, 2, BF),
+    (128, 128, 8, 260, 9, 4, 2, HF), (192, 128, 4, 300, 1, 2, 2, BF), (192, 128, 8, 130, 9, 4, 2, BF), (256, 256, 4, 300, 1, 2, 2, HF), (256, 256, 8, 130, 9, 4, 2, BF)])
+def test_more_sequences_than_blocks(dqk, dv, bits, B, Nq, H, Hkv, dtype):
+    """A wave per (sequence, KV head): short and empty sequences, a few of several chunks among them, more than 512 of them."""
+    gen = _gen(B + dqk)
+    lens = [int(x) for x in torch.randint(0, 70, (B,), generator=gen)]
+    for b in (0, B // 2, B - 1):
+        lens[b] = 1300 + b
+    _run(B, lens, Nq, H, Hkv, dqk, dv, bits, 32, dtype, True, view=bits == 8)
+
+
+def test_another_device_than_the_current_one(monkeypatch):
+    import paper_2603_05451_amd as A
+    q, f = torch.zeros(1, 8, 4, 64, dtype=BF, device="cuda"), A.attn_rope_freqs(64)
+    c = A.attn_cache_new(4, 16, 2, 64, 64)
+    i = torch.zeros(8, dtype=torch.int32, device="cuda")
+    A.lib()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+
+    class Left:                                 # (the native part asks for the device in its own way, and leaves such calls alone)
+        def __getattr__(self, name):
+            return lambda *a: None
+    monkeypatch.setattr(A, "_native", Left())
+    for call in (lambda: A.attn_rope_fwd(q, None, f), lambda: A.attn_rope_bwd(q, None, f), lambda: A.attn_cache_read(i, c, BF),
+                 lambda: A.attn_cache_write(q[0, :, :2], q[0, :, :2], i, c), lambda: A.attn_cache_fwd(q, c, i.view(1, 8), i[:1], 0.1, True),
+                 lambda: A.attn_rope_fwd(q, None, f, stream=torch.cuda.current_stream(0))):
+        with pytest.raises(ValueError, match="device"):
+            call()
+
+
 def test_wide_table_and_lengths_beyond_it():
     """A table with room for more keys than there are, and lengths that it has no room for or that are negative."""
     import paper_2603_05451_amd as A
