@@ -682,11 +682,20 @@ int check_cache_fwd(const attn_cache_t* c, int B, int Nq, int H, int table_width
     return (int64_t)s.slots * Nq * H > 0x7fffffffLL ? ATTN_EUNSUPPORTED : ATTN_OK;
 }
 
-// partial results of every chunk, if there can be more than one to a sequence
-size_t cache_parts(const attn_cache_t* c, int B, int Nq, int H, int table_width)
+// partial results of every chunk, if there can be more than one to a sequence: O | maximum and sum | where a sequence's parts are
+struct CacheParts {
+    size_t ml_off, merge_off, total;
+};
+CacheParts cache_parts(const attn_cache_t* c, int B, int Nq, int H, int table_width)
 {
     const attn::CacheShape s = attn::cache_shape(B, Nq, H, c->Hkv, c->d_qk, c->bits, (int64_t)table_width * c->page);
-    return s.slots > B ? (size_t)s.slots * Nq * H : 0;
+    if (s.slots <= B) return {0, 0, 256};
+    const size_t rows = (size_t)s.slots * Nq * H;
+    CacheParts w;
+    w.ml_off = align_up(rows * c->d_v * sizeof(float), 256);
+    w.merge_off = w.ml_off + align_up(rows * 2 * sizeof(float), 256);
+    w.total = w.merge_off + align_up((size_t)B * 4 * sizeof(int), 256);
+    return w;
 }
 
 }  // namespace
@@ -730,7 +739,7 @@ int attn_cache_read(int dtype, const attn_cache_t* cache, const int* slots, int 
 size_t attn_cache_workspace_bytes(const attn_cache_t* cache, int B, int Nq, int H, int table_width)
 {
     if (check_cache_fwd(cache, B, Nq, H, table_width) != ATTN_OK) return 0;
-    return align_up(cache_parts(cache, B, Nq, H, table_width) * (cache->d_v + 2) * sizeof(float) + 1, 256);
+    return cache_parts(cache, B, Nq, H, table_width).total;
 }
 
 int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, void* o, const attn_strides_t* so, float* lse,
@@ -744,7 +753,8 @@ int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const at
     if (!(scale > 0.0f) || !(scale < 1e30f)) return ATTN_EINVAL;
     if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4) || misaligned(block_table, 4) || misaligned(lens, 4) || misaligned(workspace, 256))
         return ATTN_EINVAL;
-    if (workspace_bytes < attn_cache_workspace_bytes(cache, B, Nq, H, table_width)) return ATTN_EINVAL;
+    const CacheParts w = cache_parts(cache, B, Nq, H, table_width);
+    if (workspace_bytes < w.total) return ATTN_EINVAL;
     attn::CacheFwdArgs a = {};
     a.c = cache_args(cache);
     a.q = q;
@@ -760,8 +770,10 @@ int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const at
     a.H = H;
     a.scale = scale;
     a.causal = causal != 0;
-    a.part_o = static_cast<float*>(workspace);
-    a.part_ml = a.part_o + cache_parts(cache, B, Nq, H, table_width) * cache->d_v;
+    char* ws = static_cast<char*>(workspace);
+    a.part_o = reinterpret_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float*>(ws + w.ml_off);
+    a.merge = reinterpret_cast<int*>(ws + w.merge_off);
     a.f16 = dtype == ATTN_F16;
     a.stream = stream;
     const int rc = attn::launch_cache_fwd(a);

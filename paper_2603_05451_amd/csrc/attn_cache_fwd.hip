@@ -83,9 +83,9 @@ struct CacheLengths {
         // tiles of a chunk: all keys in about `parts` chunks, but the mean sequence in equal ones (of 1.2 chunks it would leave most of a
         // block's or wave's time unused); whole turns of its waves, not below min_tiles
         int total = 0, used = 0;
-        each([&](int, int len) { total += (len + 31) >> 5; used += len > 0; return false; });
+        each([&](int, int len) { total += (len + 31) >> 5; used += __popcll(__ballot(len > 0)); return false; });
         total = wave_sum(total);
-        const uint32_t even = (uint32_t)(total + p.parts - 1) / p.parts, mean = (uint32_t)total / max(wave_sum(used), 1);
+        const uint32_t even = (uint32_t)(total + p.parts - 1) / p.parts, mean = (uint32_t)total / max(used, 1);
         const uint32_t n = (4 * mean + even) / max(4 * even, 1u);                      // mean / even, less a quarter, rounded
         chunk_tiles = max(((int)(n ? (mean + n - 1) / n : even) + p.waves - 1) & -p.waves, p.min_tiles);
         per_chunk = 1.0f / (float)chunk_tiles;
@@ -109,11 +109,10 @@ struct CacheLengths {
             const CacheSplit s = split(b0 + (threadIdx.x & 63), len);
             n[0] += s.whole;
 #pragma unroll
-            for (int c = 1; c < 5; ++c) n[c] += s.rest == c;
+            for (int c = 1; c < 5; ++c) n[c] += __popcll(__ballot(s.rest == c));
             return false;
         });
-#pragma unroll
-        for (int c = 0; c < 5; ++c) n[c] = wave_sum(n[c]);
+        n[0] = wave_sum(n[0]);
     }
 };
 
@@ -149,32 +148,6 @@ __device__ __forceinline__ bool cache_place(const CachePlanArgs& p, const int* _
     });
     return true;
 }
-// The chunks of sequence b, and, if there are more than one, the places of its first whole one and of its shorter one (-1: there is none).
-__device__ __forceinline__ int cache_places_of(const CachePlanArgs& p, const int* __restrict__ lens, int b, int& slot0, int& rest)
-{
-    const CacheLengths all(p, lens);
-    const CacheSplit mine = all.split(b, all.fetch(b));
-    const int chunks = mine.whole + (mine.rest > 0);
-    if (chunks == 1) return 1;
-    int n[5], before = 0, same = 0;                         // whole chunks and shorter ones of the same kind of the sequences before b
-    all.count(n);
-    all.each([&](int b0, int len) {
-        const int i = b0 + (threadIdx.x & 63);
-        const CacheSplit split = all.split(i, len);
-        if (i < b) { before += split.whole; same += split.rest == mine.rest; }
-        return false;
-    });
-    slot0 = wave_sum(before);
-    rest = -1;
-    if (mine.rest) {
-        rest = wave_sum(same);
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (c < mine.rest) rest += n[c];
-    }
-    return chunks;
-}
-
 #if ATTN_F16
 #define ATTN_ELEM f16
 #define ATTN_ELEM8 f16x8

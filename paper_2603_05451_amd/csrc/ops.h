@@ -144,6 +144,7 @@ struct CacheFwdArgs {
     float scale;
     int causal;
     float *part_o, *part_ml;    // unnormalised results of chunks: [slots][Hkv][Nq * H / Hkv][d_v], and {maximum, sum} of each row
+    int* merge;                 // [B][4]: where a sequence's parts are
     bool f16;
     void* stream;
 };
