@@ -46,7 +46,8 @@ inline void rope_shapes(int tokens, int heads_q, int heads_k, int d, bool backwa
 
 // ---- attention over the cache
 
-// Blocks of 16 rows that a wave takes together: two where there are more than 16 rows (queries times heads of a group).
+// Blocks of 16 rows that a wave takes together: two where there are more than 16 rows (queries times heads of a group), which read and
+// convert the cache once and not twice (32 sequences of 4001 keys, 5 queries, H = 32/8, d = 128: 54.7 us with one, 40.9 with two).
 inline int cache_row_blocks(int Nq, int H, int Hkv) { return (int64_t)Nq * (H / Hkv) > 16 ? 2 : 1; }
 
 // Blocks of the attention kernel that a CU holds: what its registers allow (the kernel is compiled for it).
@@ -62,26 +63,31 @@ struct CacheShape {
     int slots;          // chunks at most: `parts` of three quarters of that length and one per sequence, or what the longest could have
 };
 // Where there are more (sequence, KV head, row group)s than the chip holds blocks, each is a wave's work: a block per one of them would take
-// several rounds, whose first loads and merges (5 us each) all blocks go through at the same time.
+// several rounds, whose first loads and merges all blocks go through at the same time (d = 128, 8 KV heads, 4 bits, us as blocks / as
+// waves: 300 sequences of 500 keys 53.6 / 42.6, 192 of 1000 51.1 / 47.9, 128 of 2000 68.4 / 59.0, 96 of 4001 83.7 / 84.4; below, 32 of 4001 30.7 / 33.9).
+// A chunk has 8 tiles or more, two per wave (one sequence of 1000 keys 6.7 us with 8, 5.7 with 4, 8.4 with 16; of 8000 7.2, 7.6 and 8.8), but
+// sequences that are short by the table's width are not divided: the merge, 3 us and a launch, costs more (with it / undivided, 16
+// sequences of 500 keys 10.6 / 8.6, 760 12.8 / 11.3, 1020 13.3 / 13.5; d = 256: 500 14.5 / 13.1, 760 18.0 / 17.2, 1020 18.9 / 21.4).
 inline CacheShape cache_shape(int B, int Nq, int H, int Hkv, int d_qk, int bits, int64_t most)
 {
     const int rb = cache_row_blocks(Nq, H, Hkv);
     const int64_t rows = (int64_t)Nq * (H / Hkv);
     const int64_t side = Hkv * ((rows + 16 * rb - 1) / (16 * rb)), round = 256 * cache_blocks_per_cu(d_qk, bits, rb);
+    const int64_t tiles = (most + 31) / 32;
+    const int undivided = d_qk * bits <= 512 ? 24 : 16;
     CacheShape s;
     s.waves = B * side >= round ? 1 : 4;
     const int64_t places = round * (4 / s.waves);
     s.parts = (int)(side < places ? places / side : 1);
-    s.min_tiles = 8;
-    const int64_t tiles = (most + 31) / 32, each = (tiles + s.min_tiles - 1) / s.min_tiles;
-    const int64_t most_parts = ((int64_t)s.parts * 4 + 2) / 3 + B;
+    s.min_tiles = tiles <= undivided ? undivided : 8;
+    const int64_t each = (tiles + s.min_tiles - 1) / s.min_tiles, most_parts = ((int64_t)s.parts * 4 + 2) / 3 + B;
     s.slots = (int)(B * each < most_parts ? B * each : most_parts);
     return s;
 }
 
 // Rows (query, head) that a block of the merge takes: one per d_v / 4 of its threads where a sequence has few chunks, as far as sizes
-// tell, one otherwise (B = 32, H = 32, d = 128, 4001 keys in 3 chunks: 5.2 us with 1024 blocks of a row each, 4.4 with 128 of 8; one
-// sequence of 32000 keys in 84: 5.0 us with a row's parts dealt to 8 groups of threads).
+// tell, one otherwise (48 sequences of 67 ... 7696 keys, H = 32, d = 128: 6.6 us with 1536 blocks of a row each, 5.7 with 192 of 8; 16 of 2000,
+// d = 64, 64 rows: 6.2 and 4.7; with dozens of parts to a row these are dealt to the block's 8 groups of threads).
 inline int cache_merge_rows(const CacheShape& s, int B, int d_v, int64_t most)
 {
     const int64_t each = (most + 32 * s.min_tiles - 1) / (32 * s.min_tiles), likely = 2 * (s.parts / B) + 1;
