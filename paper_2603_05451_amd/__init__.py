@@ -482,6 +482,22 @@ def _here(t, name, dtype, stream):
                          "a call's tensors and stream belong to the current device")
 
 
+def _scratch(t, stream):
+    import torch
+    _here(t, "workspace", torch.uint8, stream)
+    if not t.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 CUDA tensor")
+
+
+def _empty(shape, dtype, device, stream):
+    """A new tensor of the call's stream: what a call makes and drops is used again behind it on that stream, not on the current one."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _rows(t, name, dtype, stream, shape=None):
     """A [B, N, heads, d] or packed [T, heads, d] view as a 4-d one."""
     _here(t, name, dtype, stream)
@@ -560,11 +576,10 @@ def attn_rope_fwd(q, k, freqs, positions=None, interleaved=False, offset=0, ampl
     if k is None and k_out is not None:
         raise ValueError("k_out without k")
     rope = _rope(x, y, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, stream)
-    import torch
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=dt, device=q.device)
+        q_out = _empty(q.shape, dt, q.device, stream)
     if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=dt, device=q.device)
+        k_out = _empty(k.shape, dt, q.device, stream)
     xo = _rows(q_out, "q_out", dt, stream, q.shape)
     yo = None if k is None else _rows(k_out, "k_out", dt, stream, k.shape)
     B, N, H, d = x.shape
@@ -599,20 +614,19 @@ def attn_rope_bwd(dq, dk, freqs, positions=None, interleaved=False, offset=0, am
         raise ValueError("dk_in without dk")
     rope = _rope(g, h, freqs, positions, interleaved, offset, amplitude, eps, q_weight, k_weight, stream)
     import torch
-    new = lambda like: torch.empty(like.shape, dtype=dt, device=dq.device)
-    dq_in = new(dq) if dq_in is None else dq_in
-    dk_in = new(dk) if dk_in is None and dk is not None else dk_in
+    dq_in = _empty(dq.shape, dt, dq.device, stream) if dq_in is None else dq_in
+    dk_in = _empty(dk.shape, dt, dq.device, stream) if dk_in is None and dk is not None else dk_in
     gi = _rows(dq_in, "dq_in", dt, stream, dq.shape)
     hi = None if dk is None else _rows(dk_in, "dk_in", dt, stream, dk.shape)
     B, N, H, d = g.shape
     Hkv = 0 if h is None else h.shape[2]
-    dqw = None if q_weight is None else torch.empty(d, dtype=torch.float32, device=dq.device)
-    dkw = None if k_weight is None else torch.empty(d, dtype=torch.float32, device=dq.device)
+    dqw = None if q_weight is None else _empty((d,), torch.float32, dq.device, stream)
+    dkw = None if k_weight is None else _empty((d,), torch.float32, dq.device, stream)
     if workspace is None:
         if dqw is not None or dkw is not None:
-            workspace = torch.empty(max(_bytes("attn_rope_workspace_bytes", B, N, H, Hkv, d), 256), dtype=torch.uint8, device=dq.device)
+            workspace = _empty((max(_bytes("attn_rope_workspace_bytes", B, N, H, Hkv, d), 256),), torch.uint8, dq.device, stream)
     else:
-        _here(workspace, "workspace", torch.uint8, stream)
+        _scratch(workspace, stream)
     _check(lib().attn_rope_bwd(code, ctypes.byref(rope), g.data_ptr(), _strides(g), _address(h), _strides(h), _address(x), _strides(x),
                                _address(y), _strides(y), gi.data_ptr(), _strides(gi), _address(hi), _strides(hi), _address(dqw), _address(dkw),
                                B, N, H, Hkv, d, _address(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)))
@@ -686,7 +700,7 @@ def attn_cache_read(slots, cache, dtype, k=None, v=None, stream=None):
     T = slots.shape[0] if slots.dim() == 1 else 0
     at = _indexes(slots, "slots", (T,), stream)
     shapes = [(T, layout.Hkv, layout.d_qk), (T, layout.Hkv, layout.d_v)]
-    k, v = (torch.empty(s, dtype=dtype, device=slots.device) if t is None else t for t, s in zip((k, v), shapes))
+    k, v = (_empty(s, dtype, slots.device, stream) if t is None else t for t, s in zip((k, v), shapes))
     code = _dtype_code(k)
     for t, name, s in zip((k, v), "kv", shapes):
         _here(t, name, dtype, stream)
@@ -716,17 +730,17 @@ def attn_cache_fwd(q, cache, block_table, lens, scale, causal, o=None, lse=None,
     width = block_table.shape[1] if block_table.dim() == 2 else 0
     table, keys = _indexes(block_table, "block_table", (B, width), stream), _indexes(lens, "lens", (B,), stream)
     if o is None:
-        o = torch.empty((B, Nq, H, layout.d_v), dtype=dt, device=q.device)
+        o = _empty((B, Nq, H, layout.d_v), dt, q.device, stream)
     if lse is None:
-        lse = torch.empty((B, H, Nq), dtype=torch.float32, device=q.device)
+        lse = _empty((B, H, Nq), torch.float32, q.device, stream)
     y = _rows(o, "o", dt, stream, (B, Nq, H, layout.d_v))
     _here(lse, "lse", torch.float32, stream)
     lse_p = _dev_lse(lse, (B, H, Nq), "B,H,Nq")
     if workspace is None:
         need = lib().attn_cache_workspace_bytes(ctypes.byref(layout), B, Nq, H, width)
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        workspace = _empty((max(need, 256),), torch.uint8, q.device, stream)
     else:
-        _here(workspace, "workspace", torch.uint8, stream)
+        _scratch(workspace, stream)
     _check(lib().attn_cache_fwd(code, ctypes.byref(layout), x.data_ptr(), _strides(x), y.data_ptr(), _strides(y), lse_p, table, width, keys,
                                 B, Nq, H, float(scale), int(bool(causal)), workspace.data_ptr(), workspace.numel(), _stream(stream)))
     return o, lse

@@ -796,6 +796,6 @@ const char* attn_strerror(int code)
     }
 }
 
-int attn_version(void) { return 100; }
+int attn_version(void) { return 200; }
 
 }  // extern "C"

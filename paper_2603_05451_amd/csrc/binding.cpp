@@ -545,7 +545,7 @@ PyObject* rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     at::Tensor gi, hi, wq, wk, ws;
     if (a[12] != Py_None) { const at::Tensor* t = c.tensor(a[12]); if (t) { gi = *t; c.rows(t, c.type, gs); --c.nstrides; } }
     if (a[13] != Py_None) { const at::Tensor* t = c.tensor(a[13]); if (t) { hi = *t; c.rows(t, c.type, hs); --c.nstrides; } }
-    if (a[14] != Py_None) { const at::Tensor* t = c.tensor(a[14]); if (t) { ws = *t; if (t->scalar_type() != at::kByte) c.ok = false; } }
+    if (a[14] != Py_None) { const at::Tensor* t = c.tensor(a[14]); if (t) { ws = *t; if (t->scalar_type() != at::kByte || !t->is_contiguous()) c.ok = false; } }
     if (!c.ok) NOT_HERE;
     const bool sums = r.q_weight || r.k_weight;
     const size_t need = sums && !ws.defined() ? p_rope_bytes(z.B, z.N, z.H, z.Hkv, z.d) : 0;
@@ -671,7 +671,7 @@ PyObject* cache_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     at::Tensor o, lse, ws;
     if (a[6] != Py_None) { const at::Tensor* t = c.tensor(a[6]); if (t) o = *t; }
     if (a[7] != Py_None) { const at::Tensor* t = c.tensor(a[7]); c.flat(t, at::kFloat, ls); if (t) lse = *t; }
-    if (a[8] != Py_None) { const at::Tensor* t = c.tensor(a[8]); if (t) { ws = *t; if (ws.scalar_type() != at::kByte) c.ok = false; } }
+    if (a[8] != Py_None) { const at::Tensor* t = c.tensor(a[8]); if (t) { ws = *t; if (t->scalar_type() != at::kByte || !t->is_contiguous()) c.ok = false; } }
     if (o.defined()) { c.rows(&o, c.type, os); --c.nstrides; }
     if (!c.ok) NOT_HERE;
     const size_t need = ws.defined() ? 0 : p_cache_bytes(&cache, B, Nq, H, width);
