@@ -55,10 +55,11 @@ struct CacheSplit {
     int whole, rest;            // rest: its class, 0 if there is none
 };
 
-// What every wave of a launch finds out from the lengths, a sequence per lane; those of the first 512 sequences are loaded at once and
+// What every wave of a launch finds out from the lengths, a sequence per lane; those of the first 64 HELD sequences are loaded at once and
 // stay in registers (300 sequences of 500 keys, 8 heads, d = 128: 58 us with the loads of 64 sequences one after the other, three times).
+// HELD = 1 is for up to 64 sequences: the code of the others, which a launch would have to fetch past, costs 0.3 ... 0.6 us.
+template <int HELD>
 struct CacheLengths {
-    static constexpr int HELD = 8;
     const CachePlanArgs& p;
     const int* __restrict__ lens;
     int held[HELD], chunk_tiles;
@@ -70,8 +71,9 @@ struct CacheLengths {
     template <typename F>
     __device__ __forceinline__ void each(F&& f) const
     {
+        if (f(0, held[0]) || HELD == 1) return;
 #pragma unroll
-        for (int i = 0; i < HELD; ++i)
+        for (int i = 1; i < HELD; ++i)
             if (64 * i >= p.B || f(64 * i, held[i])) return;
         for (int b0 = 64 * HELD; b0 < p.B; b0 += 64)
             if (f(b0, fetch(b0 + (threadIdx.x & 63)))) return;
@@ -79,7 +81,7 @@ struct CacheLengths {
     __device__ __forceinline__ CacheLengths(const CachePlanArgs& plan, const int* __restrict__ l) : p(plan), lens(l)
     {
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) held[i] = 64 * i < p.B ? fetch(64 * i + (threadIdx.x & 63)) : 0;
+        for (int i = 0; i < HELD; ++i) held[i] = HELD == 1 || 64 * i < p.B ? fetch(64 * i + (threadIdx.x & 63)) : 0;
         // tiles of a chunk: all keys in about `parts` chunks, but the mean sequence in equal ones (of 1.2 chunks it would leave most of a
         // block's or wave's time unused); whole turns of its waves, not below min_tiles
         int total = 0, used = 0;
@@ -119,9 +121,10 @@ struct CacheLengths {
 // The sequence and chunk at place `slot` of all chunks: kind by kind, in the sequences' order within a kind.  The longest first, so that the
 // shorter ones fill up what the others leave (48 sequences of 67 ... 7696 keys, 8 heads, d = 128, 4 bits: 24.8 us with the shorter chunks in
 // the sequences' order, 21.5 so; 19.5 where all have the mean length).  False behind the last chunk.
-__device__ __forceinline__ bool cache_place(const CachePlanArgs& p, const int* __restrict__ lens, int slot, CachePlace& at)
+template <int HELD>
+__device__ __forceinline__ bool cache_place_among(const CachePlanArgs& p, const int* __restrict__ lens, int slot, CachePlace& at)
 {
-    const CacheLengths all(p, lens);
+    const CacheLengths<HELD> all(p, lens);
     at.chunk_tiles = all.chunk_tiles;
     int n[5], kind = 0;
     all.count(n);
@@ -148,6 +151,11 @@ __device__ __forceinline__ bool cache_place(const CachePlanArgs& p, const int* _
     });
     return true;
 }
+__device__ __forceinline__ bool cache_place(const CachePlanArgs& p, const int* __restrict__ lens, int slot, CachePlace& at)
+{
+    return p.B <= 64 ? cache_place_among<1>(p, lens, slot, at) : cache_place_among<8>(p, lens, slot, at);
+}
+
 #if ATTN_F16
 #define ATTN_ELEM f16
 #define ATTN_ELEM8 f16x8
