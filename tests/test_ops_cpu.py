@@ -194,7 +194,7 @@ void t_cache(int B, int Nq, int H, int Hkv, int d, int bits, long long most, int
 void t_rope(int tokens, int heads, int d, int sums, int* out)
 {
     const RopeShape s = rope_shape(tokens, heads, d, sums);
-    out[0] = s.blocks; out[1] = s.hg_shift; out[2] = s.shares; out[3] = rope_lanes(d);
+    out[0] = s.blocks; out[1] = s.hg_shift; out[2] = s.shares; out[3] = rope_lanes(d); out[4] = s.rows;
 }
 }
 """
@@ -241,12 +241,12 @@ def test_rows_of_rotary_calls_are_all_taken(rules):
     r = random.Random(2)
     for _ in range(300):
         tokens, heads, d, sums = int(2 ** r.uniform(0, 12)), r.randint(1, 80), r.choice([64, 96, 128, 192, 256]), r.randint(0, 1)
-        blocks, shift, shares, lanes, _ = rules("t_rope", tokens, heads, d, sums)
+        blocks, shift, shares, lanes, turn = rules("t_rope", tokens, heads, d, sums)
         assert lanes * 16 >= d and blocks % shares == 0 and blocks > 0
         if sums:
             assert blocks <= 512 + shares
-        slots, turn, units, hg = 64 // lanes, 2 if sums else 4, 4 * (blocks // shares), 1 << shift
-        assert hg <= slots
+        slots, units, hg = 64 // lanes, 4 * (blocks // shares), 1 << shift
+        assert hg <= slots and 1 <= turn <= (2 if sums else 4)
         if tokens * heads > 4000:
             continue
         seen = set()
