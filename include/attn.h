@@ -334,6 +334,8 @@ int attn_cache_read(int dtype, const attn_cache_t* cache, const int* slots, int 
  *     its range.
  *   - Lengths and pages are read on the device: a captured call may be replayed with others.  Any Nq works; it is meant for few
  *     (one token, a few drafted ones): a long chunk reads its keys back (attn_cache_read) for attn_varlen_fwd.
+ *     B is 65536 at most, and meant to be up to some thousands: every block finds its keys from all lengths.  Sizes whose blocks (16 or
+ *     32 rows of a KV head and a sequence, four of those where there are many) pass 2^22 are ATTN_EUNSUPPORTED.
  *   workspace: attn_cache_workspace_bytes(...) bytes, 256-byte aligned, contents ignored.  One kernel, and a merge where the table
  *   is wide enough for a sequence to be divided. */
 size_t attn_cache_workspace_bytes(const attn_cache_t* cache, int B, int Nq, int H, int table_width);

@@ -677,9 +677,10 @@ int check_cache_fwd(const attn_cache_t* c, int B, int Nq, int H, int table_width
     if (B <= 0 || Nq <= 0 || H <= 0 || table_width <= 0 || H % c->Hkv != 0) return ATTN_EINVAL;
     const int64_t most = (int64_t)table_width * c->page;
     if (most > 0x7fffffffLL - 31 || B * ((most + 31) / 32) > (1 << 29)) return ATTN_EUNSUPPORTED;
-    if ((int64_t)Nq * H > (1 << 24) || (int64_t)B * Nq * H > 0x7fffffffLL) return ATTN_EUNSUPPORTED;
+    if (B > 65536 || (int64_t)Nq * H > (1 << 24) || (int64_t)B * Nq * H > 0x7fffffffLL) return ATTN_EUNSUPPORTED;
     const attn::CacheShape s = attn::cache_shape(B, Nq, H, c->Hkv, c->d_qk, c->bits, most);
-    return (int64_t)s.slots * Nq * H > 0x7fffffffLL ? ATTN_EUNSUPPORTED : ATTN_OK;
+    if ((int64_t)s.slots * Nq * H > 0x7fffffffLL || attn::cache_fwd_blocks(s, Nq, H, c->Hkv) > attn::kMostBlocks) return ATTN_EUNSUPPORTED;
+    return attn::cache_merge_blocks(s, B, Nq, H, c->d_v, most) > attn::kMostBlocks ? ATTN_EUNSUPPORTED : ATTN_OK;
 }
 
 // partial results of every chunk, if there can be more than one to a sequence: O | maximum and sum | where a sequence's parts are

@@ -10,6 +10,9 @@ namespace attn {
 // Lanes of a wave that hold one row: two chunks of 8 dims each, a power of two.
 inline int rope_lanes(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 
+// Blocks of one launch at most, for a quarter of the 2^32 threads that it may have (the rotary calls have one for q and one for k).
+constexpr int kMostBlocks = 1 << 22;
+
 // Rows of a lane whose loads are in flight together.
 constexpr int rope_rows(bool backward) { return backward ? 2 : 4; }
 
@@ -37,6 +40,8 @@ inline RopeShape rope_shape(int tokens, int heads, int d, bool backward)
     if (waves() * singles <= 1024) { r.rows = 1; r.shares = singles; }
     else if (waves() < 1024) r.shares = (singles + r.rows - 1) / r.rows;
     int64_t groups = (waves() + 3) / 4;
+    if (r.shares > kMostBlocks) r.shares = kMostBlocks;
+    if (groups * r.shares > kMostBlocks) groups = kMostBlocks / r.shares;
     if (backward && groups * r.shares > 512) groups = (512 + r.shares - 1) / r.shares;      // partial sums per block
     r.blocks = (int)(groups * r.shares);
     return r;
@@ -96,6 +101,19 @@ inline int cache_merge_rows(const CacheShape& s, int B, int d_v, int64_t most)
 {
     const int64_t each = (most + 32 * s.min_tiles - 1) / (32 * s.min_tiles), likely = 2 * (s.parts / B) + 1;
     return (each < likely ? each : likely) <= 16 ? 1024 / d_v : 1;
+}
+
+// Blocks of the attention kernel, and of the merge.
+inline int64_t cache_fwd_blocks(const CacheShape& s, int Nq, int H, int Hkv)
+{
+    const int rows = 16 * cache_row_blocks(Nq, H, Hkv);
+    const int64_t units = (int64_t)s.slots * Hkv * (((int64_t)Nq * (H / Hkv) + rows - 1) / rows);
+    return s.waves == 4 ? units : (units + 3) / 4;
+}
+inline int64_t cache_merge_blocks(const CacheShape& s, int B, int Nq, int H, int d_v, int64_t most)
+{
+    const int per = cache_merge_rows(s, B, d_v, most);
+    return B * (((int64_t)Nq * H + per - 1) / per);
 }
 
 }  // namespace attn

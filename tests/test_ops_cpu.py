@@ -114,6 +114,21 @@ def test_cache_attention_refusals(L):
     assert size(3, 1, 8, 4) == 256 and size(3, 1, 8, 100) > 256 and size(3, 1, 7, 4) == 0 and size(3, 1, 8, 4, bits=3) == 0
 
 
+def test_launches_within_the_grid(L, rules):
+    """Sizes whose blocks would be more than a launch takes are refused, or their rows dealt to fewer blocks."""
+    import paper_2603_05451_amd as A
+    size = lambda *a, **c: L.attn_cache_workspace_bytes(ctypes.byref(_cache(**c)), *a)
+    assert size(65536, 1, 8, 4) > 0 and size(65537, 1, 8, 4) == 0 and size(1 << 20, 1, 64, 1) == 0
+    assert size(60000, 1, 512, 64, Hkv=512) == 0 and size(60000, 64, 128, 64) == 0 and size(1, 1 << 20, 16, 1000) > 0
+    x = _st(1 << 20, 128, 128)
+    s = lambda B, H: L.attn_cache_fwd(0, ctypes.byref(_cache(Hkv=H)), P, x, P, x, P, P, 4, P, B, 1, H, 0.1, 1, P, 1 << 60, None)
+    assert s(65537, 2) == A.ATTN_EUNSUPPORTED and s(60000, 1024) == A.ATTN_EUNSUPPORTED
+    for tokens, heads in ((1 << 30, 1), (1 << 30, 2), (1023, 1 << 20), (1, 1 << 20)):
+        for d in (64, 256):
+            blocks, _, shares, _, _ = rules("t_rope", tokens, heads, d, 0)
+            assert 0 < blocks <= 1 << 22 and blocks % shares == 0
+
+
 def test_python_refusals_without_a_gpu():
     import paper_2603_05451_amd as A
     t = torch.zeros(1, 4, 2, 64, dtype=torch.bfloat16)
