@@ -270,8 +270,8 @@ int attn_bwd_strided(int dtype, const void* q, const attn_strides_t* sq, const v
  * exact: far positions lose nothing; A = amplitude.  Contexts longer than trained ones are a matter of freqs and amplitude.
  * positions: int32, one per token, any value, token n of sequence b at positions[b * positions_batch + n] (positions_batch = 0: the
  * same for every sequence); null: n.  Sums and products are in fp32; the result is rounded once, to the element type.
- *   tensors: views as in attn_fwd_strided, q and q_out [B, N, H, d], k and k_out [B, N, Hkv, d] (B = 1 for packed tokens), d 64,
- *   96, 128, 192 or 256; k and k_out may both be null.  An output may be its input (same address and strides); any other overlap
+ *   tensors: views as in attn_fwd_strided, the token stride without its limit, q and q_out [B, N, H, d], k and k_out
+ *   [B, N, Hkv, d] (B = 1 for packed tokens), d 64, 96, 128, 192 or 256; k and k_out may both be null.  An output may be its input (same address and strides); any other overlap
  *   is an error of the caller's. */
 typedef struct attn_rope {
     const float* freqs;         /* [rot / 2], fp32, device */
@@ -312,7 +312,7 @@ typedef struct attn_cache {
     void *k, *k_scale, *v, *v_scale;
     int pages, page, Hkv, d_qk, d_v, bits;
 } attn_cache_t;
-/* Quantises k [T, Hkv, d_qk] and v [T, Hkv, d_v] (token and head strides; `batch` is not used) into the slots slots[0 ... T-1] (int32,
+/* Quantises k [T, Hkv, d_qk] and v [T, Hkv, d_v] (views as in attn_rope_fwd; `batch` is not used) into the slots slots[0 ... T-1] (int32,
  * device).  A row whose slot is negative or past the cache is skipped (padding); the others must differ, or the bytes of a slot that is
  * given twice are unspecified.  No other byte of the cache is touched. */
 int attn_cache_write(int dtype, const attn_cache_t* cache, const void* k, const attn_strides_t* sk, const void* v, const attn_strides_t* sv,
@@ -322,7 +322,7 @@ int attn_cache_write(int dtype, const attn_cache_t* cache, const void* k, const 
  * is infinite beyond its range. */
 int attn_cache_read(int dtype, const attn_cache_t* cache, const int* slots, int T, void* k, void* v, void* stream);
 /* Attention of Nq queries per sequence over that cache: sequence b has lens[b] keys (int32, device), key j in page
- * block_table[b * table_width + j / page] (int32, device) at j % page.  q and o are views [B, Nq, H, d] as in attn_fwd_strided, lse [B, H, Nq]
+ * block_table[b * table_width + j / page] (int32, device) at j % page.  q and o are views [B, Nq, H, d] as in attn_rope_fwd, lse [B, H, Nq]
  * contiguous.  causal != 0: the last query is aligned with the last key (key j visible to query i iff j <= i + lens[b] - Nq).
  *   - A query without a visible key (an empty batch slot, lens[b] = 0, or causal with fewer keys than queries) has o = 0 and
  *     lse = -inf.  A negative length counts as 0, one beyond table_width * page as that.

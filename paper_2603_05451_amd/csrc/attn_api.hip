@@ -411,14 +411,16 @@ int check_strided(int B, int H, int Hkv, int Nq, int Nk, int d_qk, int d_v)
 
 // every stride a multiple of 8 elements (16 bytes: vector loads and the global->LDS copies),
 // rows and heads apart (stride 0 only where there is a single one)
-bool bad_stride(const attn_strides_t* s, int B, int N, int heads)
+bool bad_view(const attn_strides_t* s, int B, int N, int heads)
 {
     if (!s) return true;
     if (s->batch % 8 || s->row % 8 || s->head % 8) return true;
     if (s->batch < 0 || s->row < 0 || s->head < 0) return true;
-    if ((B > 1 && s->batch == 0) || (N > 1 && s->row == 0) || (heads > 1 && s->head == 0)) return true;
-    if (s->row > (1LL << 23)) return true;     // byte offsets inside a 128-row tile are 32-bit
-    return false;
+    return (B > 1 && s->batch == 0) || (N > 1 && s->row == 0) || (heads > 1 && s->head == 0);
+}
+bool bad_stride(const attn_strides_t* s, int B, int N, int heads)
+{
+    return bad_view(s, B, N, heads) || s->row > (1LL << 23);       // byte offsets inside a 128-row tile are 32-bit
 }
 
 // rows and batches back to back: the layout of the fixed-length calls (the stride of an axis with one entry is not used)
@@ -573,8 +575,8 @@ int attn_rope_fwd(int dtype, const attn_rope_t* rope, const void* q, const attn_
     if (int rc = check_rope(dtype, rope, both, B, N, H, Hkv, d)) return rc;
     if (!q || !q_out || both != (k_out != nullptr)) return ATTN_EINVAL;
     if (misaligned(q, 16) || misaligned(k, 16) || misaligned(q_out, 16) || misaligned(k_out, 16)) return ATTN_EINVAL;
-    if (bad_stride(sq, B, N, H) || bad_stride(sqo, B, N, H)) return ATTN_EINVAL;
-    if (both && (bad_stride(sk, B, N, Hkv) || bad_stride(sko, B, N, Hkv))) return ATTN_EINVAL;
+    if (bad_view(sq, B, N, H) || bad_view(sqo, B, N, H)) return ATTN_EINVAL;
+    if (both && (bad_view(sk, B, N, Hkv) || bad_view(sko, B, N, Hkv))) return ATTN_EINVAL;
     attn::RopeArgs a = rope_args(dtype, rope, B, N, H, both ? Hkv : 0, d, stream);
     a.x[0] = q;
     a.x[1] = k;
@@ -611,8 +613,8 @@ int attn_rope_bwd(int dtype, const attn_rope_t* rope, const void* dq, const attn
     for (const void* p : ptrs)
         if (misaligned(p, 16)) return ATTN_EINVAL;
     if (misaligned(dq_weight, 4) || misaligned(dk_weight, 4) || misaligned(workspace, 256)) return ATTN_EINVAL;
-    if (bad_stride(sdq, B, N, H) || bad_stride(sdqi, B, N, H) || (norm && bad_stride(sq, B, N, H))) return ATTN_EINVAL;
-    if (both && (bad_stride(sdk, B, N, Hkv) || bad_stride(sdki, B, N, Hkv) || (norm && bad_stride(sk, B, N, Hkv)))) return ATTN_EINVAL;
+    if (bad_view(sdq, B, N, H) || bad_view(sdqi, B, N, H) || (norm && bad_view(sq, B, N, H))) return ATTN_EINVAL;
+    if (both && (bad_view(sdk, B, N, Hkv) || bad_view(sdki, B, N, Hkv) || (norm && bad_view(sk, B, N, Hkv)))) return ATTN_EINVAL;
     if (sums && (!workspace || workspace_bytes < attn_rope_workspace_bytes(B, N, H, both ? Hkv : 0, d))) return ATTN_EINVAL;
     attn::RopeArgs a = rope_args(dtype, rope, B, N, H, both ? Hkv : 0, d, stream);
     a.sign = -1.0f;
@@ -706,7 +708,7 @@ int attn_cache_write(int dtype, const attn_cache_t* cache, const void* k, const 
 {
     if (int rc = check_cache_rows(dtype, cache, slots, T)) return rc;
     if (!k || !v || misaligned(k, 16) || misaligned(v, 16)) return ATTN_EINVAL;
-    if (bad_stride(sk, 1, T, cache->Hkv) || bad_stride(sv, 1, T, cache->Hkv)) return ATTN_EINVAL;
+    if (bad_view(sk, 1, T, cache->Hkv) || bad_view(sv, 1, T, cache->Hkv)) return ATTN_EINVAL;
     attn::CacheRowsArgs a = {};
     a.c = cache_args(cache);
     a.xk = k;
@@ -750,7 +752,7 @@ int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const at
     if (dtype != ATTN_BF16 && dtype != ATTN_F16) return ATTN_EUNSUPPORTED;
     if (!q || !o || !lse || !block_table || !lens || !workspace) return ATTN_EINVAL;
     if (int rc = check_cache_fwd(cache, B, Nq, H, table_width)) return rc;
-    if (bad_stride(sq, B, Nq, H) || bad_stride(so, B, Nq, H)) return ATTN_EINVAL;
+    if (bad_view(sq, B, Nq, H) || bad_view(so, B, Nq, H)) return ATTN_EINVAL;
     if (!(scale > 0.0f) || !(scale < 1e30f)) return ATTN_EINVAL;
     if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4) || misaligned(block_table, 4) || misaligned(lens, 4) || misaligned(workspace, 256))
         return ATTN_EINVAL;

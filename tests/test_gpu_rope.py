@@ -146,6 +146,24 @@ def test_in_place_packed_and_one_tensor():
     assert got[0] is g[0] and all(torch.equal(x, y) for x, y in zip(got[:3], want[:3]))
 
 
+def test_offsets_beyond_32_bits():
+    """Tokens further apart than 2^31 elements, and a sequence behind that; inputs, gradients and outputs."""
+    import paper_2603_05451_amd as A
+    gen = _gen(5)
+    f, w = A.attn_rope_freqs(64), torch.rand(64, generator=gen).to(BF).cuda()
+    x, dy = (torch.randn(2, 2, 3, 64, generator=gen).to(BF).cuda() for _ in range(2))
+    far = torch.empty((1 << 32) + (1 << 20), dtype=BF, device="cuda").as_strided((2, 2, 3, 64), ((1 << 31) + 512, 1 << 31, 64, 1))
+    want = A.attn_rope_fwd(x, None, f, eps=1e-6, q_weight=w)[0]
+    back = A.attn_rope_bwd(dy, None, f, eps=1e-6, q=x, q_weight=w)
+    far.copy_(x)
+    assert torch.equal(A.attn_rope_fwd(far, None, f, eps=1e-6, q_weight=w)[0], want)
+    assert torch.equal(A.attn_rope_bwd(dy, None, f, eps=1e-6, q=far, q_weight=w)[0], back[0])
+    assert torch.equal(A.attn_rope_fwd(x, None, f, eps=1e-6, q_weight=w, q_out=far)[0], want)
+    far.copy_(dy)
+    got = A.attn_rope_bwd(far, None, f, eps=1e-6, q=x, q_weight=w, dq_in=far)
+    assert got[0] is far and torch.equal(far, back[0]) and torch.equal(got[2], back[2])
+
+
 def test_zero_rows_and_rows_that_are_no_numbers():
     """A row of zeros has a finite norm; one NaN or infinity stays in its own row."""
     import paper_2603_05451_amd as A
