@@ -271,8 +271,8 @@ int attn_bwd_strided(int dtype, const void* q, const attn_strides_t* sq, const v
  * positions: int32, one per token, any value, token n of sequence b at positions[b * positions_batch + n] (positions_batch = 0: the
  * same for every sequence); null: n.  Sums and products are in fp32; the result is rounded once, to the element type.
  *   tensors: views as in attn_fwd_strided, the token stride without its limit, q and q_out [B, N, H, d], k and k_out
- *   [B, N, Hkv, d] (B = 1 for packed tokens), d 64, 96, 128, 192 or 256; k and k_out may both be null.  An output may be its input (same address and strides); any other overlap
- *   is an error of the caller's. */
+ *   [B, N, Hkv, d] (B = 1 for packed tokens), d 64, 96, 128, 192 or 256; k and k_out may both be null.  An output may be
+ *   its input (same address and strides); any other overlap is an error of the caller's. */
 typedef struct attn_rope {
     const float* freqs;         /* [rot / 2], fp32, device */
     const int* positions;       /* device, or null */
