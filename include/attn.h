@@ -328,10 +328,12 @@ int attn_cache_read(int dtype, const attn_cache_t* cache, const int* slots, int 
  *     lse = -inf.  A negative length counts as 0, one beyond table_width * page as that.
  *   - Entries of the table behind a sequence's last key are not read.  A page number outside the cache makes the rows that see
  *     its keys NaN; nothing outside the tensors is touched.
- *   - A block of a key or value that is NaN (scale byte 255) reaches the queries that see it and no others; what the slots behind
- *     the last key hold (never written, another sequence's, NaN) reaches none.  (e4m3's own NaN, 0x7f, which attn_cache_write does
- *     not write, may reach earlier queries of the call.)  For fp16 queries the cache's numbers are taken as fp16: infinite beyond
- *     its range.
+ *   - Keys and values that are no finite numbers (a scale byte of 255; e4m3's own NaN, 0x7f, which attn_cache_write does not write;
+ *     for fp16 queries, whose type the cache's numbers are taken in, what is beyond its range) reach the queries that see them and no
+ *     others: a value makes its channel of their o infinite or NaN, a key all of it.  What the slots behind the last key hold (never
+ *     written, another sequence's, NaN) reaches none.
+ *   - Sums are in fp32, o's before their division by the row sum, with weights up to 2^8: finite values of 2^120 / lens[b] and more may
+ *     make it infinite.
  *   - Lengths and pages are read on the device: a captured call may be replayed with others.  Any Nq works; it is meant for few
  *     (one token, a few drafted ones): a long chunk reads its keys back (attn_cache_read) for attn_varlen_fwd.
  *     B is 65536 at most, and meant to be up to some thousands: every block finds its keys from all lengths.  Sizes whose blocks (16 or

@@ -43,4 +43,19 @@ __device__ __forceinline__ E8 cache_e4m3(E e, uint32_t w0, uint32_t w1, float sc
     return __builtin_bit_cast(E8, u32x4{e4m3_pair<false>(e, w0, scale), e4m3_pair<true>(e, w0, scale), e4m3_pair<false>(e, w1, scale), e4m3_pair<true>(e, w1, scale)});
 }
 
+// Whether 16 bytes of codes under this scale byte may hold numbers that are infinite or NaN as element type E (4 * 2^126 and 256 * 2^120
+// are 2^128, 4 * 2^14 and 256 * 2^8 are 2^16; e4m3 has a NaN of its own).
+template <int BITS, typename E>
+__device__ __forceinline__ bool cache_odd(E, const uint32_t (&w)[4], uint32_t byte)
+{
+    constexpr bool f16_ = std::is_same_v<E, f16>;
+    constexpr uint32_t finite = BITS == 4 ? (f16_ ? 140 : 252) : (f16_ ? 134 : 246);        // the largest scale without
+    bool odd = byte > finite;
+    if constexpr (BITS == 8) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= (((w[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+    }
+    return odd;
+}
+
 }  // namespace attn
