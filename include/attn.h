@@ -269,7 +269,8 @@ int attn_bwd_strided(int dtype, const void* q, const attn_strides_t* sq, const v
  * dims (offset + p, offset + rot/2 + p), or, with interleaved != 0, (offset + 2p, offset + 2p + 1); a = position * freqs[p], as if
  * exact: far positions lose nothing; A = amplitude.  Contexts longer than trained ones are a matter of freqs and amplitude.
  * positions: int32, one per token, any value, token n of sequence b at positions[b * positions_batch + n] (positions_batch = 0: the
- * same for every sequence); null: n.  Sums and products are in fp32; the result is rounded once, to the element type.
+ * same for every sequence); null: n.  Sums and products are in fp32, with the power of two that a row takes whose squares would leave
+ * its range; the result is rounded once, to the element type.  A row of zeros is NaN with eps = 0, zeros otherwise.
  *   tensors: views as in attn_fwd_strided, the token stride without its limit, q and q_out [B, N, H, d], k and k_out
  *   [B, N, Hkv, d] (B = 1 for packed tokens), d 64, 96, 128, 192 or 256; k and k_out may both be null.  An output may be
  *   its input (same address and strides); any other overlap is an error of the caller's. */
