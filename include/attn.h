@@ -319,8 +319,9 @@ typedef struct attn_cache {
 int attn_cache_write(int dtype, const attn_cache_t* cache, const void* k, const attn_strides_t* sk, const void* v, const attn_strides_t* sv,
                      const int* slots, int T, void* stream);
 /* The rows of these slots (any order, any number of times) as numbers of the element type: k [T, Hkv, d_qk], v [T, Hkv, d_v], contiguous;
- * zeros where a slot is negative or past the cache.  bf16 holds every value that was written from 16-bit numbers; fp16 rounds and
- * is infinite beyond its range. */
+ * zeros where a slot is negative or past the cache.  bf16 holds every value exactly but 2^128, which is infinite: what a number of at
+ * least 7 * 2^125 (2.98e38; 4 bits) or 248 * 2^120 (3.30e38; 8 bits) was rounded to.  fp16 rounds, and is infinite from 2^16 on: of its own
+ * numbers, those of at least 57344 (4 bits) or 63488 (8 bits). */
 int attn_cache_read(int dtype, const attn_cache_t* cache, const int* slots, int T, void* k, void* v, void* stream);
 /* Attention of Nq queries per sequence over that cache: sequence b has lens[b] keys (int32, device), key j in page
  * block_table[b * table_width + j / page] (int32, device) at j % page.  q and o are views [B, Nq, H, d] as in attn_rope_fwd, lse [B, H, Nq]

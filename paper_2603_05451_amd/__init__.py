@@ -690,7 +690,8 @@ def attn_cache_write(k, v, slots, cache, stream=None):
 
 
 def attn_cache_read(slots, cache, dtype, k=None, v=None, stream=None):
-    """The rows at slots int32 [T] as bf16 or fp16 -> (k [T,Hkv,d_qk], v [T,Hkv,d_v]); zeros where a slot is negative or past the cache."""
+    """The rows at slots int32 [T] as bf16 or fp16 -> (k [T,Hkv,d_qk], v [T,Hkv,d_v]); zeros where a slot is negative or past the cache,
+    infinite where a value is beyond the type's range (include/attn.h: numbers near its end that were rounded up)."""
     import torch
     if dtype is torch.bfloat16 or dtype is torch.float16:
         r = (_native or _call()).cache_read(slots, cache, dtype is torch.float16, k, v, stream)

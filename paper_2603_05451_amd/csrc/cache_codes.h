@@ -1,6 +1,6 @@
 // Codes of the quantised cache as pairs of 16-bit numbers (gfx950's conversions).  They take the scale as a float whose exponent
 // field is the scale byte: 2^(byte - 127), byte 0 included; a byte of 255 gives NaN.  They round to the element type: bf16 holds
-// every value exactly, fp16 is as a conversion from fp32 would be (infinite beyond its range).
+// every value below 2^128 exactly, fp16 is as a conversion from fp32 would be; both are infinite beyond their range.
 #pragma once
 #include "common.h"
 
