@@ -308,7 +308,7 @@ int attn_rope_bwd(int dtype, const attn_rope_t* rope, const void* dq, const attn
  * of the block is cut off when it is rounded to nearest (ties to even); a block that holds an infinity or a NaN is NaN.  Rounding
  * is exact arithmetic: codes and scales depend on the row's values alone.
  *   page: tokens per page, a power of two, 16 ... 65536; pages * page <= 2^31 - 1; head dims as elsewhere.
- * Slot s is token s % page of page s / page.  Calls on rows take T * Hkv * d up to 2^34 - 2048. */
+ * Slot s is token s % page of page s / page.  Calls on rows take T of at least 1 and T * Hkv * d up to 2^34 - 2048. */
 typedef struct attn_cache {
     void *k, *k_scale, *v, *v_scale;
     int pages, page, Hkv, d_qk, d_v, bits;
@@ -341,7 +341,7 @@ int attn_cache_read(int dtype, const attn_cache_t* cache, const int* slots, int 
  *     B is 65536 at most, and meant to be up to some thousands: every block finds its keys from all lengths.  Sizes whose blocks (16 or
  *     32 rows of a KV head and a sequence, four of those where there are many) pass 2^22 are ATTN_EUNSUPPORTED.
  *   workspace: attn_cache_workspace_bytes(...) bytes, 256-byte aligned, contents ignored.  One kernel, and a merge where the table
- *   is wide enough for a sequence to be divided. */
+ *   is wide enough for a sequence to be divided (without which the o and lse of divided sequences are untouched). */
 size_t attn_cache_workspace_bytes(const attn_cache_t* cache, int B, int Nq, int H, int table_width);
 int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, void* o, const attn_strides_t* so, float* lse,
                    const int* block_table, int table_width, const int* lens, int B, int Nq, int H, float scale, int causal,

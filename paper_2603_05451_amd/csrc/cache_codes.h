@@ -40,7 +40,8 @@ __device__ __forceinline__ E8 cache_e2m1(E e, uint32_t w, float scale)
 template <typename E8, typename E>
 __device__ __forceinline__ E8 cache_e4m3(E e, uint32_t w0, uint32_t w1, float scale)
 {
-    return __builtin_bit_cast(E8, u32x4{e4m3_pair<false>(e, w0, scale), e4m3_pair<true>(e, w0, scale), e4m3_pair<false>(e, w1, scale), e4m3_pair<true>(e, w1, scale)});
+    return __builtin_bit_cast(E8, u32x4{e4m3_pair<false>(e, w0, scale), e4m3_pair<true>(e, w0, scale),
+                                        e4m3_pair<false>(e, w1, scale), e4m3_pair<true>(e, w1, scale)});
 }
 
 // Whether 16 bytes of codes under this scale byte may hold numbers that are infinite or NaN as element type E (4 * 2^126 and 256 * 2^120

@@ -59,10 +59,20 @@ inline void rope_shapes(int tokens, int heads_q, int heads_k, int d, bool backwa
 // convert the cache once and not twice (32 sequences of 4001 keys, 5 queries, H = 32/8, d = 128: 54.7 us with one, 40.9 with two).
 inline int cache_row_blocks(int Nq, int H, int Hkv) { return (int64_t)Nq * (H / Hkv) > 16 ? 2 : 1; }
 
-// Blocks of the attention kernel that a CU holds: what its registers allow (the kernel is compiled for it).
+// Blocks of the attention kernel that a CU holds, which it is compiled for: what its registers allow without spilling more than a few.
+// 32 sequences of 8000 keys, H = 32/8, us with one block fewer (where it is not one) / so / one more, with one and with two row blocks:
+//   d = 64          4 bits 42 / 39 / 40, 58 / 53 / 51       8 bits 56 / 56 / 76, 66 / 62 / 93
+//   d = 96                 66 / 56 / 77, 122 / 77 / 132            111 / 81 / 87, 128 / 89 / 257
+//   d = 128                65 / 61 / 76, 113 / 81 / 197            138 / 102 / 132, 161 / 112 / 342
+//   d = (192, 128)         112 / 75 / 75, 126 / 92 / 357           130 / 129 / 250, - / 162 / 216
+//   d = 256                136 / 111 / 584, - / 188 / 632          - / 205 / 496, - / 231 / 1044
 constexpr int cache_blocks_per_cu(int d_qk, int bits, int row_blocks)
 {
-    return d_qk > 192 ? (bits == 4 && row_blocks == 1 ? 2 : 1) : d_qk > 128 ? (bits == 8 && row_blocks == 2 ? 1 : 2) : d_qk > 64 ? (bits == 4 && row_blocks == 1 ? 3 : 2) : row_blocks == 1 ? 4 : 3;
+    const bool lean = bits == 4 && row_blocks == 1;
+    if (d_qk > 192) return lean ? 2 : 1;
+    if (d_qk > 128) return bits == 8 && row_blocks == 2 ? 1 : 2;
+    if (d_qk > 64) return lean ? 3 : 2;
+    return row_blocks == 1 ? 4 : 3;
 }
 
 struct CacheShape {
@@ -72,8 +82,12 @@ struct CacheShape {
     int slots;          // chunks at most: `parts` of three quarters of that length and one per sequence, or what the longest could have
 };
 // Where there are more (sequence, KV head, row group)s than the chip holds blocks, each is a wave's work: a block per one of them would take
-// several rounds, whose first loads and merges all blocks go through at the same time (d = 128, 8 KV heads, 4 bits, us as blocks / as
-// waves: 300 sequences of 500 keys 53.6 / 42.6, 192 of 1000 51.1 / 47.9, 128 of 2000 68.4 / 59.0, 96 of 4001 83.7 / 84.4; below, 32 of 4001 30.7 / 33.9).
+// several rounds, whose first loads and merges all blocks go through at the same time (4 bits, 8 KV heads, one row block, us as blocks / as
+// waves: d = 128 300 sequences of 500 keys 53.6 / 42.6, 192 of 1000 51.1 / 47.9, 128 of 2000 68.4 / 59.0; d = 96 100 of 1000 33.2 / 31.3; d = 256
+// 200 of 500 70.3 / 58.9; 8 bits: d = 128 100 of 2000 97 / 90, d = 96 100 of 1000 46 / 41; below one round 32 of 4001 30.7 / 33.9).  The line
+// could lie higher: units for just one round are the faster as blocks (d = 128 96 of 4001 83.7 / 84.4, 8 bits 64 of 4001 98.6 / 101.7; d = 64
+// 128 of 2000 36.4 / 38; d = 192 64 of 2000 43.5 / 45.5), and with two row blocks those for 1.5 as well (32 sequences, 64 rows, 300 keys 15.1 / 22.2,
+// 1000 26.5 / 33.7, 8000 134 / 140; 128 rows 236 / 242, 8 bits 317 / 315; 96 of 2000, 32 rows 74 / 83).
 // A chunk has 8 tiles or more, two per wave (one sequence of 1000 keys 6.7 us with 8, 5.7 with 4, 8.4 with 16; of 8000 7.2, 7.6 and 8.8), but
 // sequences that are short by the table's width are not divided: the merge, 3 us and a launch, costs more (with it / undivided, 16
 // sequences of 500 keys 10.6 / 8.6, 760 12.8 / 11.3, 1020 13.3 / 13.5; d = 256: 500 14.5 / 13.1, 760 18.0 / 17.2, 1020 18.9 / 21.4).
