@@ -347,6 +347,52 @@ int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const at
                    const int* block_table, int table_width, const int* lens, int B, int Nq, int H, float scale, int causal,
                    void* workspace, size_t workspace_bytes, void* stream);
 
+/* Attention of chunks of queries over that cache: sequence b has the queries cu_seqlens[b] ... cu_seqlens[b + 1] - 1 of q (packed [T, H, d_qk], int32
+ * [B + 1], device) and lens[b] keys in the pages of its row of block_table, as in attn_cache_fwd; with a chunk of a prompt these are what was
+ * cached before and the chunk itself, already written.  q and o are views [T, H, d] as in attn_rope_fwd (`batch` is not used), lse [H, T]
+ * contiguous.  causal != 0: a sequence's last query is aligned with its last key (key j visible to its query i iff j <= i + lens[b] - queries).
+ *   - Empty queries, lengths, pages and numbers that are not finite are dealt with as in attn_cache_fwd, whatever the chunk's length.
+ *   - A sequence whose boundaries do not ascend within 0 ... T has no queries.  Rows of q that belong to no sequence (padding behind the last
+ *     one) are not touched in o and lse.  Two sequences must not share queries (the results of such rows are unspecified).
+ *   - Boundaries, lengths and pages are read on the device: a captured call may be replayed with others.
+ *     B is 65536 at most, T * H * d up to 2^34, T * H up to 2^28.
+ *   workspace: attn_cache_chunk_workspace_bytes(...) bytes, 256-byte aligned, contents ignored.  One kernel, and a merge where there are so few rows
+ *   that keys may be divided over blocks (without which the o and lse of divided sequences are untouched). */
+size_t attn_cache_chunk_workspace_bytes(const attn_cache_t* cache, int B, int T, int H);
+int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, void* o, const attn_strides_t* so, float* lse,
+                         const int* block_table, int table_width, const int* cu_seqlens, const int* lens, int B, int T, int H, float scale, int causal,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* The attention weight that every cached key had from the queries of one of these calls, added to its sum: weights is fp32 [pages, Hkv, page],
+ * contiguous, 16-byte aligned, one per row of the cache, and
+ *     weights(j) += sum over the sequence's queries i that see key j, and the heads h of the KV head's group, of exp(scale q_ih . k_j - lse_ih),
+ * for every key j < lens[b] of every sequence that has queries.  q and lse are that call's: with cu_seqlens those of attn_cache_chunk_fwd (q packed,
+ * Nq is T, lse [H, T]), with cu_seqlens null those of attn_cache_fwd (q [B, Nq, H, d_qk], lse [B, H, Nq]).
+ *   - fresh != 0: the sequence's last keys, as many as it has queries, are the call's own: their weights are set, not added to, so that
+ *     what a page held before does not matter.
+ *   - A query with lse = -inf (it saw no key) adds nothing.  A key that is not finite has the weight NaN.  Entries of the table that are
+ *     outside the cache are passed over.  Weights of other rows are not touched.
+ *   - Every row of the cache may belong to one sequence at most (a page that two sequences share has unspecified weights).
+ *   - Sums are in fp32, in an order that depends on the sizes and lengths alone.  One kernel, no workspace.  Limits as in the two calls. */
+int attn_cache_weigh(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, const float* lse, float* weights,
+                     const int* block_table, int table_width, const int* cu_seqlens, const int* lens, int B, int Nq, int H, float scale, int causal,
+                     int fresh, void* stream);
+
+/* Eviction by those weights: of every sequence with more than keep[b] rows (int32, device; a negative number counts as 0) that many stay, for each KV
+ * head by itself: the last `recent` (no more than keep[b]), and of the others those with the greatest weights (ties: the first; NaN is the greatest,
+ * -0 and 0 are equal).  The cache is closed up in place, rows with their weights: with n = keep[b] - recent, survivors below n remain where they
+ * are, the others go, in ascending order, to the places below n that are free, the recent rows, in order, to n ... keep[b] - 1.  So rows change
+ * their places, which attention does not mind (keys hold their positions), and few rows are moved; the last ones remain in order.  What lies behind
+ * the first keep[b] rows is left as it is, and its pages are free.  lens_out[b] = min(lens[b], keep[b]); lens_out may not be lens or keep.
+ *   - Lengths as in attn_cache_fwd.  A row of a page number outside the cache has the least weight; one that stays nevertheless is NaN, with weight 0, where
+ *     it goes to a place in the cache.
+ *   - Every row of the cache may belong to one sequence at most.
+ *   - B * Hkv is 2^22 at most.
+ *   workspace: attn_cache_evict_workspace_bytes(...) bytes (4 for every row that the table has room for, and head), 256-byte aligned, contents ignored. */
+size_t attn_cache_evict_workspace_bytes(const attn_cache_t* cache, int B, int table_width);
+int attn_cache_evict(const attn_cache_t* cache, float* weights, const int* block_table, int table_width, const int* lens, const int* keep, int recent,
+                     int B, int* lens_out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Software 2^x of paper Sec. 3.1.3 (range reduction + degree-n minimax polynomial, p0 = 1, Horner
  * with FMAs, exponent splice), provided to measure its accuracy on this hardware; attn_fwd does not
  * use it (v_exp_f32 and the FMAs share one issue port on CDNA4, so emulation cannot add throughput:

@@ -99,6 +99,16 @@ def lib():
         L.attn_cache_workspace_bytes.restype = sz
         L.attn_cache_fwd.argtypes = [i, cp, vp, sp, vp, sp, vp, vp, i, vp, i, i, i, f, i, vp, sz, vp]
         L.attn_cache_fwd.restype = i
+        L.attn_cache_chunk_workspace_bytes.argtypes = [cp, i, i, i]
+        L.attn_cache_chunk_workspace_bytes.restype = sz
+        L.attn_cache_chunk_fwd.argtypes = [i, cp, vp, sp, vp, sp, vp, vp, i, vp, vp, i, i, i, f, i, vp, sz, vp]
+        L.attn_cache_chunk_fwd.restype = i
+        L.attn_cache_weigh.argtypes = [i, cp, vp, sp, vp, vp, vp, i, vp, vp, i, i, i, f, i, i, vp]
+        L.attn_cache_weigh.restype = i
+        L.attn_cache_evict_workspace_bytes.argtypes = [cp, i, i]
+        L.attn_cache_evict_workspace_bytes.restype = sz
+        L.attn_cache_evict.argtypes = [cp, vp, vp, i, vp, vp, i, i, vp, vp, sz, vp]
+        L.attn_cache_evict.restype = i
         L.attn_exp2_emulated.argtypes = [vp, vp, sz, i, vp]
         L.attn_exp2_emulated.restype = i
         L.attn_strerror.argtypes = [i]
@@ -113,7 +123,9 @@ def lib():
         _binding.bind(*(address(f) for f in (L.attn_fwd_dtype, L.attn_bwd_phases, L.attn_bwd_dtype, L.attn_bwd_workspace_bytes, L.attn_varlen_fwd_dtype,
                                              L.attn_varlen_bwd_dtype, L.attn_varlen_workspace_bytes, L.attn_fwd_strided, L.attn_bwd_strided,
                                              L.attn_strided_workspace_bytes, L.attn_rope_fwd, L.attn_rope_bwd, L.attn_rope_workspace_bytes,
-                                             L.attn_cache_write, L.attn_cache_read, L.attn_cache_fwd, L.attn_cache_workspace_bytes)),
+                                             L.attn_cache_write, L.attn_cache_read, L.attn_cache_fwd, L.attn_cache_workspace_bytes,
+                                             L.attn_cache_chunk_fwd, L.attn_cache_chunk_workspace_bytes, L.attn_cache_weigh, L.attn_cache_evict,
+                                             L.attn_cache_evict_workspace_bytes)),
                       torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.nn.Parameter)
         _native = _binding
         _lib = L                # last: another thread that finds it set uses both
@@ -745,3 +757,110 @@ def attn_cache_fwd(q, cache, block_table, lens, scale, causal, o=None, lse=None,
     _check(lib().attn_cache_fwd(code, ctypes.byref(layout), x.data_ptr(), _strides(x), y.data_ptr(), _strides(y), lse_p, table, width, keys,
                                 B, Nq, H, float(scale), int(bool(causal)), workspace.data_ptr(), workspace.numel(), _stream(stream)))
     return o, lse
+
+
+def attn_cache_chunk_workspace_bytes(cache, B, T, H) -> int:
+    return int(lib().attn_cache_chunk_workspace_bytes(ctypes.byref(_cache(cache, None)), B, T, H))
+
+
+def attn_cache_chunk_fwd(q, cache, block_table, cu_seqlens, lens, scale, causal, o=None, lse=None, workspace=None, stream=None):
+    """Attention of chunks of new tokens over a paged cache: q [T,H,d_qk] (a view with a contiguous last axis) holds the queries of sequence b in rows
+    cu_seqlens[b] ... cu_seqlens[b+1] - 1 (int32 [B+1]); lens int32 [B] counts its keys (the chunk's own among them, written before), key j in page
+    block_table[b, j // page] (int32 [B,width]); under the causal mask a sequence's last query sees its last key.
+    -> (o [T,H,d_v], lse [H,T] fp32); a query without a visible key has o = 0 and lse = -inf, rows of no sequence are not touched (unspecified in new
+    tensors)."""
+    r = (_native or _call()).cache_chunk_fwd(q, cache, block_table, cu_seqlens, lens, scale, causal, o, lse, workspace, stream)
+    if r is not None:
+        return _done(r)
+    import torch
+    layout = _cache(cache, stream)
+    code, dt = _dtype_code(q), q.dtype
+    if q.dim() != 3:
+        raise ValueError("q must be a [T, H, d] tensor")
+    T, H, _ = q.shape
+    x = _rows(q, "q", dt, stream, (T, H, layout.d_qk))
+    B, width = block_table.shape if block_table.dim() == 2 else (0, 0)
+    table, keys = _indexes(block_table, "block_table", (B, width), stream), _indexes(lens, "lens", (B,), stream)
+    cu = _indexes(cu_seqlens, "cu_seqlens", (B + 1,), stream)
+    if o is None:
+        o = _empty((T, H, layout.d_v), dt, q.device, stream)
+    if lse is None:
+        lse = _empty((H, T), torch.float32, q.device, stream)
+    y = _rows(o, "o", dt, stream, (T, H, layout.d_v))
+    _here(lse, "lse", torch.float32, stream)
+    lse_p = _dev_lse(lse, (H, T), "H,T")
+    if workspace is None:
+        workspace = _empty((max(lib().attn_cache_chunk_workspace_bytes(ctypes.byref(layout), B, T, H), 256),), torch.uint8, q.device, stream)
+    else:
+        _scratch(workspace, stream)
+    _check(lib().attn_cache_chunk_fwd(code, ctypes.byref(layout), x.data_ptr(), _strides(x), y.data_ptr(), _strides(y), lse_p, table, width, cu, keys,
+                                      B, T, H, float(scale), int(bool(causal)), workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    return o, lse
+
+
+def attn_cache_weights(cache):
+    """Weights of a cache's rows for attn_cache_weigh and attn_cache_evict: zeros, fp32 [pages, Hkv, page]."""
+    import torch
+    return torch.zeros(cache[0].shape[:3], dtype=torch.float32, device=cache[0].device)
+
+
+def _weights(weights, layout, stream):
+    import torch
+    _here(weights, "weights", torch.float32, stream)
+    return _dev(weights, "weights", (layout.pages, layout.Hkv, layout.page), torch.float32)
+
+
+def attn_cache_weigh(q, lse, weights, cache, block_table, lens, scale, causal, cu_seqlens=None, fresh=False, stream=None):
+    """Adds to weights (fp32 [pages,Hkv,page], attn_cache_weights) the attention weight that each key of the sequences had from the queries of an
+    attn_cache_chunk_fwd call (q [T,H,d_qk], its lse [H,T], its cu_seqlens) or an attn_cache_fwd call (q [B,Nq,H,d_qk], its lse [B,H,Nq], no
+    cu_seqlens), summed over queries and the heads of a KV head's group; the other arguments are that call's.  fresh: the last keys, as many as the
+    sequence has queries, are the call's own, their weights are set and not added to.  -> weights"""
+    r = (_native or _call()).cache_weigh(q, lse, weights, cache, block_table, lens, scale, causal, cu_seqlens, fresh, stream)
+    if r is not None:
+        _check(r)
+        return weights
+    import torch
+    layout = _cache(cache, stream)
+    code, dt = _dtype_code(q), q.dtype
+    if q.dim() != (4 if cu_seqlens is None else 3):
+        raise ValueError("q must be a [T, H, d] tensor with cu_seqlens, a [B, Nq, H, d] tensor without")
+    x = _rows(q, "q", dt, stream, (*q.shape[:-1], layout.d_qk))
+    B, width = block_table.shape if block_table.dim() == 2 else (0, 0)
+    table, keys = _indexes(block_table, "block_table", (B, width), stream), _indexes(lens, "lens", (B,), stream)
+    N, H = q.shape[-3], q.shape[-2]
+    if cu_seqlens is None and q.shape[0] != B:
+        raise ValueError(f"q has {q.shape[0]} sequences, block_table {B}")
+    cu = None if cu_seqlens is None else _indexes(cu_seqlens, "cu_seqlens", (B + 1,), stream)
+    _here(lse, "lse", torch.float32, stream)
+    lse_p = _dev_lse(lse, (B, H, N), "B,H,Nq") if cu is None else _dev_lse(lse, (H, N), "H,T")
+    _check(lib().attn_cache_weigh(code, ctypes.byref(layout), x.data_ptr(), _strides(x), lse_p, _weights(weights, layout, stream), table, width, cu, keys,
+                                  B, N, H, float(scale), int(bool(causal)), int(bool(fresh)), _stream(stream)))
+    return weights
+
+
+def attn_cache_evict_workspace_bytes(cache, B, table_width) -> int:
+    return int(lib().attn_cache_evict_workspace_bytes(ctypes.byref(_cache(cache, None)), B, table_width))
+
+
+def attn_cache_evict(weights, cache, block_table, lens, keep, recent, lens_out=None, workspace=None, stream=None):
+    """Cuts the sequences of a paged cache down to keep[b] rows (int32 [B]), for every KV head by itself: the last `recent` stay and, of the others, those
+    of greatest weight.  Rows and weights are moved in place to the sequence's first keep[b] places (which goes where: include/attn.h); the pages
+    behind them are free.  -> lens_out int32 [B], min(lens, keep) (not lens itself)"""
+    r = (_native or _call()).cache_evict(weights, cache, block_table, lens, keep, recent, lens_out, workspace, stream)
+    if r is not None:
+        return _done(r)
+    import torch
+    layout = _cache(cache, stream)
+    B, width = block_table.shape if block_table.dim() == 2 else (0, 0)
+    table, keys = _indexes(block_table, "block_table", (B, width), stream), _indexes(lens, "lens", (B,), stream)
+    w, k = _weights(weights, layout, stream), _indexes(keep, "keep", (B,), stream)
+    if lens_out is None:
+        lens_out = _empty((B,), torch.int32, lens.device, stream)
+    out = _indexes(lens_out, "lens_out", (B,), stream)
+    if workspace is None:
+        workspace = _empty((max(lib().attn_cache_evict_workspace_bytes(ctypes.byref(layout), B, width), 256),), torch.uint8, lens.device, stream)
+    else:
+        _scratch(workspace, stream)
+    _check(lib().attn_cache_evict(ctypes.byref(layout), w, table, width, keys, k, int(recent), B, out, workspace.data_ptr(), workspace.numel(),
+                                  _stream(stream)))
+    return lens_out

@@ -39,6 +39,9 @@ SOURCES = [*[("attn_bwd_dq_q64.hip", f"attn_bwd_dq_q64_{f16}{varlen}.o", [f"-DAT
            ("attn_rope.hip", "attn_rope.o", []),
            ("attn_cache.hip", "attn_cache.o", []),
            *[("attn_cache_fwd.hip", f"attn_cache_fwd_{f16}.o", [f"-DATTN_F16={f16}", *VGPR_FORM]) for f16 in (0, 1)],
+           *[("attn_cache_chunk.hip", f"attn_cache_chunk_{f16}.o", [f"-DATTN_F16={f16}", *VGPR_FORM]) for f16 in (0, 1)],
+           ("attn_cache_weigh.hip", "attn_cache_weigh.o", VGPR_FORM),
+           ("attn_cache_evict.hip", "attn_cache_evict.o", []),
            ("exp2_emulated.hip", "exp2_emulated.o", [])]
 PROBE_SOURCES = [("probes.hip", "probes.o", [])]
 # packed-fp32 instruction selection is switched off on purpose (device passes only; the

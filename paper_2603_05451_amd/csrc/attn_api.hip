@@ -783,6 +783,153 @@ int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const at
     return rc == 0 ? ATTN_OK : (rc == -2 ? ATTN_EUNSUPPORTED : ATTN_ELAUNCH);
 }
 
+namespace {
+
+// a cache with its table, B sequences and heads
+int check_cache_table(const attn_cache_t* c, int B, int H, int table_width)
+{
+    if (int rc = check_cache(c)) return rc;
+    if (B <= 0 || H <= 0 || table_width <= 0 || H % c->Hkv != 0) return ATTN_EINVAL;
+    const int64_t most = (int64_t)table_width * c->page;
+    return most > 0x7fffffffLL - 1024 || B > 65536 ? ATTN_EUNSUPPORTED : ATTN_OK;
+}
+
+int check_cache_chunk(const attn_cache_t* c, int B, int T, int H)
+{
+    if (int rc = check_cache_table(c, B, H, 1)) return rc;
+    if (T <= 0) return ATTN_EINVAL;
+    if ((int64_t)T * H > 1 << 28 || (int64_t)T * H * (c->d_qk > c->d_v ? c->d_qk : c->d_v) > 1LL << 34) return ATTN_EUNSUPPORTED;
+    const attn::ChunkShape s = attn::chunk_shape(B, T, H, c->Hkv, c->d_qk);
+    return s.units * c->Hkv > attn::kMostBlocks || (int64_t)T * H * c->d_v / 1024 >= attn::kMostBlocks ? ATTN_EUNSUPPORTED : ATTN_OK;
+}
+
+// partial results of every block, if there may be more than one to a row tile: O | maximum and sum
+size_t chunk_part_rows(const attn_cache_t* c, int B, int T, int H)
+{
+    const attn::ChunkShape s = attn::chunk_shape(B, T, H, c->Hkv, c->d_qk);
+    return s.places == 0 ? 0 : (size_t)s.units * c->Hkv * attn::kChunkRows;
+}
+
+}  // namespace
+
+size_t attn_cache_chunk_workspace_bytes(const attn_cache_t* cache, int B, int T, int H)
+{
+    if (check_cache_chunk(cache, B, T, H) != ATTN_OK) return 0;
+    const size_t rows = chunk_part_rows(cache, B, T, H);
+    return rows == 0 ? 256 : rows * (cache->d_v + 2) * sizeof(float);
+}
+
+int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, void* o, const attn_strides_t* so, float* lse,
+                         const int* block_table, int table_width, const int* cu_seqlens, const int* lens, int B, int T, int H, float scale, int causal,
+                         void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (dtype != ATTN_BF16 && dtype != ATTN_F16) return ATTN_EUNSUPPORTED;
+    if (!q || !o || !lse || !block_table || !cu_seqlens || !lens || !workspace) return ATTN_EINVAL;
+    if (int rc = check_cache_table(cache, B, H, table_width)) return rc;
+    if (int rc = check_cache_chunk(cache, B, T, H)) return rc;
+    if (bad_view(sq, 1, T, H) || bad_view(so, 1, T, H)) return ATTN_EINVAL;
+    if (!(scale > 0.0f) || !(scale < 1e30f)) return ATTN_EINVAL;
+    if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4) || misaligned(block_table, 4) || misaligned(cu_seqlens, 4) || misaligned(lens, 4) ||
+        misaligned(workspace, 256))
+        return ATTN_EINVAL;
+    if (workspace_bytes < attn_cache_chunk_workspace_bytes(cache, B, T, H)) return ATTN_EINVAL;
+    attn::CacheChunkArgs a = {};
+    a.c = cache_args(cache);
+    a.q = q;
+    a.o = o;
+    a.lse = lse;
+    a.q_row = sq->row;
+    a.q_head = sq->head;
+    a.o_row = so->row;
+    a.o_head = so->head;
+    a.table = block_table;
+    a.cu = cu_seqlens;
+    a.lens = lens;
+    a.table_width = table_width;
+    a.B = B;
+    a.T = T;
+    a.H = H;
+    a.scale = scale;
+    a.causal = causal != 0;
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = a.part_o + chunk_part_rows(cache, B, T, H) * cache->d_v;
+    a.f16 = dtype == ATTN_F16;
+    a.stream = stream;
+    const int rc = attn::launch_cache_chunk(a);
+    return rc == 0 ? ATTN_OK : (rc == -2 ? ATTN_EUNSUPPORTED : ATTN_ELAUNCH);
+}
+
+int attn_cache_weigh(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, const float* lse, float* weights,
+                     const int* block_table, int table_width, const int* cu_seqlens, const int* lens, int B, int Nq, int H, float scale, int causal,
+                     int fresh, void* stream)
+{
+    if (dtype != ATTN_BF16 && dtype != ATTN_F16) return ATTN_EUNSUPPORTED;
+    if (!q || !lse || !weights || !block_table || !lens) return ATTN_EINVAL;
+    if (int rc = check_cache_table(cache, B, H, table_width)) return rc;
+    if (Nq <= 0) return ATTN_EINVAL;
+    const int64_t T = cu_seqlens ? Nq : (int64_t)B * Nq;
+    if (T * H > 1 << 28 || T * H * cache->d_qk > 1LL << 34) return ATTN_EUNSUPPORTED;
+    if (attn::weigh_units(B, cache->Hkv, cache->d_qk, (int64_t)table_width * cache->page) > 1 << 30) return ATTN_EUNSUPPORTED;
+    if (bad_view(sq, cu_seqlens ? 1 : B, Nq, H)) return ATTN_EINVAL;
+    if (!(scale > 0.0f) || !(scale < 1e30f)) return ATTN_EINVAL;
+    if (misaligned(q, 16) || misaligned(lse, 4) || misaligned(weights, 16) || misaligned(block_table, 4) || misaligned(cu_seqlens, 4) || misaligned(lens, 4))
+        return ATTN_EINVAL;
+    attn::CacheWeighArgs a = {};
+    a.c = cache_args(cache);
+    a.q = q;
+    a.lse = lse;
+    a.weights = weights;
+    a.sq = as_is(sq);
+    a.lse_batch = cu_seqlens ? 0 : (long long)H * Nq;
+    a.lse_head = Nq;
+    a.table = block_table;
+    a.lens = lens;
+    a.cu = cu_seqlens;
+    a.table_width = table_width;
+    a.B = B;
+    a.Nq = Nq;
+    a.T = (int)T;
+    a.H = H;
+    a.scale = scale;
+    a.causal = causal != 0;
+    a.fresh = fresh != 0;
+    a.f16 = dtype == ATTN_F16;
+    a.stream = stream;
+    const int rc = attn::launch_cache_weigh(a);
+    return rc == 0 ? ATTN_OK : (rc == -2 ? ATTN_EUNSUPPORTED : ATTN_ELAUNCH);
+}
+
+size_t attn_cache_evict_workspace_bytes(const attn_cache_t* cache, int B, int table_width)
+{
+    if (check_cache_table(cache, B, cache ? cache->Hkv : 0, table_width) != ATTN_OK || (int64_t)B * cache->Hkv > attn::kMostBlocks) return 0;
+    return align_up((size_t)B * (size_t)cache->Hkv * (size_t)attn::evict_ints((int64_t)table_width * cache->page) * sizeof(int), 256);
+}
+
+int attn_cache_evict(const attn_cache_t* cache, float* weights, const int* block_table, int table_width, const int* lens, const int* keep, int recent,
+                     int B, int* lens_out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!weights || !block_table || !lens || !keep || !lens_out || !workspace) return ATTN_EINVAL;
+    if (int rc = check_cache_table(cache, B, cache ? cache->Hkv : 0, table_width)) return rc;
+    if (recent < 0 || lens_out == lens || lens_out == keep) return ATTN_EINVAL;
+    if ((int64_t)B * cache->Hkv > attn::kMostBlocks) return ATTN_EUNSUPPORTED;
+    if (misaligned(weights, 16) || misaligned(block_table, 4) || misaligned(lens, 4) || misaligned(keep, 4) || misaligned(lens_out, 4) || misaligned(workspace, 256))
+        return ATTN_EINVAL;
+    if (workspace_bytes < attn_cache_evict_workspace_bytes(cache, B, table_width)) return ATTN_EINVAL;
+    attn::CacheEvictArgs a = {};
+    a.c = cache_args(cache);
+    a.weights = weights;
+    a.table = block_table;
+    a.lens = lens;
+    a.keep = keep;
+    a.lens_out = lens_out;
+    a.table_width = table_width;
+    a.B = B;
+    a.recent = recent;
+    a.places = static_cast<int*>(workspace);
+    a.stream = stream;
+    return attn::launch_cache_evict(a) == 0 ? ATTN_OK : ATTN_ELAUNCH;
+}
+
 const char* attn_strerror(int code)
 {
     switch (code) {

@@ -1,0 +1,158 @@
+// Attention of chunks of new tokens over a paged cache in 4 or 8 bits (gfx950): attn_cache_chunk_fwd of include/attn.h.  How: at the top
+// of attn_cache_chunk_kernel.inc.  ATTN_F16 names the element type of this object: one of the two per compilation.
+#include "cache_codes.h"
+#include "common.h"
+#include "launch.h"
+#include "ops.h"
+#include "wave_sums.h"
+
+namespace attn {
+namespace {
+
+// ---- which rows and keys a block takes, from the boundaries and lengths in device memory
+struct ChunkPlanArgs {
+    int B, T, G, Hkv, page_shift, most;     // most: keys that a row of the table has room for
+    int tile_keys, places, min_tiles;       // chunk_shape's; places = 0: no sequence's keys are divided
+};
+// A sequence: its first query, number of queries (0: there is nothing to do) and of keys.
+struct ChunkSeq {
+    int q0, nq, len;
+};
+struct ChunkPlace {
+    ChunkSeq s;
+    int b;                                  // its index
+    int rt, part, parts, part_tiles, unit;  // row tile; which of the parts of its keys, of so many key tiles; index of that part's unit
+};
+
+// What every wave of a launch finds out, a sequence per lane (the first 64 stay in registers).
+struct ChunkWork {
+    const ChunkPlanArgs& p;
+    const int* __restrict__ cu;
+    const int* __restrict__ lens;
+    ChunkSeq held;
+    int part_tiles;
+
+    __device__ __forceinline__ ChunkSeq fetch(int b) const
+    {
+        if (b >= p.B) return {0, 0, 0};
+        const int q0 = cu[b], q1 = cu[b + 1];
+        const bool inside = q0 >= 0 && q1 > q0 && q1 <= p.T;               // others are not acted on
+        return {q0, inside ? q1 - q0 : 0, min(max(lens[b], 0), p.most)};
+    }
+    // f(sequence of the lane, its index), 64 sequences after the other, until it says true
+    template <typename F>
+    __device__ __forceinline__ void each(F&& f) const
+    {
+        const int lane = threadIdx.x & 63;
+        if (f(held, lane)) return;
+        for (int b0 = 64; b0 < p.B; b0 += 64)
+            if (f(fetch(b0 + lane), b0 + lane)) return;
+    }
+    __device__ __forceinline__ int row_tiles(const ChunkSeq& s) const { return (s.nq * p.G + kChunkRows - 1) / kChunkRows; }
+    __device__ __forceinline__ int key_tiles(const ChunkSeq& s) const { return (s.len + p.tile_keys - 1) / p.tile_keys; }
+    __device__ __forceinline__ int parts(const ChunkSeq& s) const
+    {
+        return p.places == 0 ? 1 : max(1, (key_tiles(s) + part_tiles - 1) / part_tiles);
+    }
+    __device__ __forceinline__ int units(const ChunkSeq& s) const { return row_tiles(s) * parts(s); }
+
+    // Key tiles of a part: all key tiles of all row tiles in about `places` parts (a round of blocks), longer if the sequences' last,
+    // shorter parts would make it more.
+    __device__ __forceinline__ ChunkWork(const ChunkPlanArgs& plan, const int* __restrict__ c, const int* __restrict__ l) : p(plan), cu(c), lens(l)
+    {
+        held = fetch(threadIdx.x & 63);
+        part_tiles = 1;
+        if (p.places == 0) return;
+        float total = 0.f;
+        each([&](const ChunkSeq& s, int) { total += (float)row_tiles(s) * (float)key_tiles(s); return false; });
+        total = wave_sum(total);
+        const int places = max(1, p.places / p.Hkv);
+        part_tiles = max(p.min_tiles, (int)ceilf(total / (float)places));
+        for (int i = 0; i < 3; ++i) {
+            int n = 0;
+            each([&](const ChunkSeq& s, int) { n += units(s); return false; });
+            n = wave_sum(n);
+            if (n <= places) break;
+            part_tiles += max(1, part_tiles / 4);
+        }
+    }
+    // The sequence and its part that unit u is; false behind the last one.
+    __device__ __forceinline__ bool find(int u, ChunkPlace& at) const
+    {
+        bool found = false;
+        int before = 0;
+        each([&](const ChunkSeq& s, int b) {
+            const int mine = units(s), upto = before + wave_prefix(mine);
+            const uint64_t past = __ballot(upto > u);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+                at.s = {of(s.q0), of(s.nq), of(s.len)};
+                at.b = of(b);
+                place(at, u - (of(upto) - of(mine)));
+                at.unit = u;
+                return found = true;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+            return false;
+        });
+        return found;
+    }
+    // Unit `local` of its sequence: part by part of the keys, in each the row tiles from the last, whose loops are the longest under the
+    // mask, to the first.
+    __device__ __forceinline__ void place(ChunkPlace& at, int local) const
+    {
+        const int rts = row_tiles(at.s), tiles = key_tiles(at.s);
+        at.parts = parts(at.s);
+        at.part = local / rts;
+        at.rt = rts - 1 - (local - at.part * rts);
+        at.part_tiles = (tiles + at.parts - 1) / at.parts;
+    }
+    // The sequence of query t, and the unit of the first part of the row tile of its row `row_in_query` (with all its parts a `stride` apart).
+    __device__ __forceinline__ bool find_query(int t, int row_in_query, ChunkPlace& at, int& row, int& stride) const
+    {
+        bool found = false;
+        int before = 0;
+        each([&](const ChunkSeq& s, int) {
+            const int mine = units(s), upto = before + wave_prefix(mine);
+            const uint64_t here = __ballot(s.nq > 0 && t >= s.q0 && t < s.q0 + s.nq);
+            if (here) {
+                const int l = __builtin_ctzll(here);
+                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+                at.s = {of(s.q0), of(s.nq), of(s.len)};
+                row = (t - at.s.q0) * p.G + row_in_query;
+                at.rt = row / kChunkRows;
+                at.parts = parts(at.s);
+                at.part_tiles = (key_tiles(at.s) + at.parts - 1) / at.parts;
+                stride = row_tiles(at.s);
+                at.unit = of(upto) - of(mine) + stride - 1 - at.rt;
+                return found = true;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+            return false;
+        });
+        return found;
+    }
+};
+
+#if ATTN_F16
+#define ATTN_ELEM f16
+#define ATTN_ELEM8 f16x8
+#define ATTN_ELEM4 f16x4
+#else
+#define ATTN_ELEM bf16
+#define ATTN_ELEM8 bf16x8
+#define ATTN_ELEM4 bf16x4
+#endif
+#include "elem.inc"
+#include "attn_cache_chunk_kernel.inc"
+
+}  // namespace
+
+#if ATTN_F16
+int launch_cache_chunk_f16(const CacheChunkArgs& a) { return cache_chunk_dims(a); }
+#else
+int launch_cache_chunk_bf16(const CacheChunkArgs& a) { return cache_chunk_dims(a); }
+#endif
+
+}  // namespace attn

@@ -4,6 +4,7 @@
 #include "common.h"
 #include "launch.h"
 #include "ops.h"
+#include "wave_sums.h"
 
 namespace attn {
 namespace {
@@ -33,21 +34,6 @@ struct CachePlanArgs {
 struct CachePlace {
     int b, len, chunk, chunks, chunk_tiles;     // of a sequence; chunks of chunk_tiles 32-key tiles
 };
-
-// Inclusive prefix sums over the lanes of a wave: within 16 lanes, then the ends of rows 0 and 2 to rows 1 and 3, then that of row 1 to
-// both upper rows.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int add_moved(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
-__device__ __forceinline__ int wave_prefix(int x)
-{
-    x = add_moved<0x111, 0xf>(x);          // row_shr 1, 2, 4, 8
-    x = add_moved<0x112, 0xf>(x);
-    x = add_moved<0x114, 0xf>(x);
-    x = add_moved<0x118, 0xf>(x);
-    x = add_moved<0x142, 0xa>(x);          // row_bcast 15
-    return add_moved<0x143, 0xc>(x);       // row_bcast 31
-}
-__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
 
 // The chunks of a sequence: whole ones, and one that is shorter (also if there are no keys, for its rows have results), which is of class
 // 1 ... 4 by its length in quarters, the longest first.

@@ -32,6 +32,11 @@ decltype(&attn_cache_write) p_cache_write = nullptr;
 decltype(&attn_cache_read) p_cache_read = nullptr;
 decltype(&attn_cache_fwd) p_cache_fwd = nullptr;
 decltype(&attn_cache_workspace_bytes) p_cache_bytes = nullptr;
+decltype(&attn_cache_chunk_fwd) p_cache_chunk = nullptr;
+decltype(&attn_cache_chunk_workspace_bytes) p_chunk_bytes = nullptr;
+decltype(&attn_cache_weigh) p_cache_weigh = nullptr;
+decltype(&attn_cache_evict) p_cache_evict = nullptr;
+decltype(&attn_cache_evict_workspace_bytes) p_evict_bytes = nullptr;
 PyObject *get_device = nullptr, *get_stream = nullptr;      // torch._C._cuda_getDevice, _cuda_getCurrentRawStream
 PyTypeObject* parameter = nullptr;                          // torch.nn.Parameter
 
@@ -691,12 +696,116 @@ PyObject* cache_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// q, cache, block_table, cu_seqlens, lens, scale, causal, o, lse, workspace, stream
+PyObject* cache_chunk_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    CallHere c;
+    if (n != 11) NOT_HERE;
+    const at::Tensor *q = c.tensor(a[0]), *table = c.tensor(a[2]), *cu = c.tensor(a[3]), *lens = c.tensor(a[4]);
+    c.element(q);
+    const attn_cache_t cache = cache_of(c, a[1]);
+    if (!c.ok || q->dim() != 3 || table->dim() != 2) NOT_HERE;
+    const int T = size(q, 0), H = size(q, 1), B = size(table, 0), width = size(table, 1);
+    const double scale = c.number(a[5]);
+    const int causal = c.truth(a[6]);
+    const int64_t qs[] = {T, H, cache.d_qk}, os[] = {T, H, cache.d_v}, ts[] = {B, width}, ls[] = {H, T}, edges = (int64_t)B + 1;
+    void *qp = c.rows(q, c.type, qs), *tp = c.flat(table, at::kInt, ts), *np = c.flat(lens, at::kInt, at::IntArrayRef(ts, 1));
+    void* up = c.flat(cu, at::kInt, at::IntArrayRef(&edges, 1));
+    at::Tensor o, lse, ws;
+    if (a[7] != Py_None) { const at::Tensor* t = c.tensor(a[7]); if (t) o = *t; }
+    if (a[8] != Py_None) { const at::Tensor* t = c.tensor(a[8]); c.flat(t, at::kFloat, ls); if (t) lse = *t; }
+    if (a[9] != Py_None) { const at::Tensor* t = c.tensor(a[9]); if (t) { ws = *t; if (t->scalar_type() != at::kByte || !t->is_contiguous()) c.ok = false; } }
+    if (o.defined()) { c.rows(&o, c.type, os); --c.nstrides; }
+    if (!c.ok) NOT_HERE;
+    const size_t need = ws.defined() ? 0 : p_chunk_bytes(&cache, B, T, H);
+    void* s = c.stream_here(a[10]);
+    if (!c.ok) NOT_HERE;
+    int rc;
+    {
+        Unlocked threads;
+        if (!o.defined()) o = make(*q, {T, H, cache.d_v});
+        if (!lse.defined()) lse = make_f32(*q, {H, T});
+        if (!ws.defined()) ws = make_bytes(*q, need);
+        void* op = c.rows(&o, c.type, os);
+        rc = p_cache_chunk(c.dtype, &cache, qp, c.strides, op, c.strides + 1, (float*)lse.data_ptr(), (const int*)tp, width, (const int*)up, (const int*)np,
+                           B, T, H, (float)scale, causal, ws.data_ptr(), (size_t)ws.numel(), s);
+    }
+    return outs(rc, {{a[7], &o}, {a[8], &lse}});
+    END_HANDLE_TH_ERRORS
+}
+
+// q, lse, weights, cache, block_table, lens, scale, causal, cu_seqlens, fresh, stream
+PyObject* cache_weigh(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    CallHere c;
+    if (n != 11) NOT_HERE;
+    const at::Tensor *q = c.tensor(a[0]), *lse = c.tensor(a[1]), *weights = c.tensor(a[2]), *table = c.tensor(a[4]), *lens = c.tensor(a[5]);
+    const at::Tensor* cu = a[8] == Py_None ? nullptr : c.tensor(a[8]);
+    c.element(q);
+    const attn_cache_t cache = cache_of(c, a[3]);
+    const int packed = a[8] != Py_None;
+    if (!c.ok || q->dim() != 4 - packed || table->dim() != 2) NOT_HERE;
+    const int B = size(table, 0), width = size(table, 1), N = size(q, 1 - packed), H = size(q, 2 - packed);
+    const double scale = c.number(a[6]);
+    const int causal = c.truth(a[7]), fresh = c.truth(a[9]);
+    const int64_t qs[] = {B, N, H, cache.d_qk}, ts[] = {B, width}, ls[] = {B, H, N}, wsh[] = {cache.pages, cache.Hkv, cache.page}, edges = (int64_t)B + 1;
+    void *qp = c.rows(q, c.type, at::IntArrayRef(qs + packed, 4 - packed)), *tp = c.flat(table, at::kInt, ts), *np = c.flat(lens, at::kInt, at::IntArrayRef(ts, 1));
+    void *lp = c.flat(lse, at::kFloat, at::IntArrayRef(ls + packed, 3 - packed)), *wp = c.flat(weights, at::kFloat, wsh);
+    void* up = packed ? c.flat(cu, at::kInt, at::IntArrayRef(&edges, 1)) : nullptr;
+    void* s = c.stream_here(a[10]);
+    if (!c.ok) NOT_HERE;
+    int rc;
+    {
+        Unlocked threads;
+        rc = p_cache_weigh(c.dtype, &cache, qp, c.strides, (const float*)lp, (float*)wp, (const int*)tp, width, (const int*)up, (const int*)np, B, N, H,
+                           (float)scale, causal, fresh, s);
+    }
+    return PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// weights, cache, block_table, lens, keep, recent, lens_out, workspace, stream
+PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    CallHere c;
+    if (n != 9) NOT_HERE;
+    const at::Tensor *weights = c.tensor(a[0]), *table = c.tensor(a[2]), *lens = c.tensor(a[3]), *keep = c.tensor(a[4]);
+    const attn_cache_t cache = cache_of(c, a[1]);
+    if (!c.ok || table->dim() != 2) NOT_HERE;
+    const int B = size(table, 0), width = size(table, 1), recent = c.integer(a[5]);
+    const int64_t ts[] = {B, width}, wsh[] = {cache.pages, cache.Hkv, cache.page};
+    void *wp = c.flat(weights, at::kFloat, wsh), *tp = c.flat(table, at::kInt, ts);
+    void *np = c.flat(lens, at::kInt, at::IntArrayRef(ts, 1)), *kp = c.flat(keep, at::kInt, at::IntArrayRef(ts, 1));
+    at::Tensor left, ws;
+    if (a[6] != Py_None) { const at::Tensor* t = c.tensor(a[6]); c.flat(t, at::kInt, at::IntArrayRef(ts, 1)); if (t) left = *t; }
+    if (a[7] != Py_None) { const at::Tensor* t = c.tensor(a[7]); if (t) { ws = *t; if (t->scalar_type() != at::kByte || !t->is_contiguous()) c.ok = false; } }
+    if (!c.ok) NOT_HERE;
+    const size_t need = ws.defined() ? 0 : p_evict_bytes(&cache, B, width);
+    void* s = c.stream_here(a[8]);
+    if (!c.ok) NOT_HERE;
+    int rc;
+    {
+        Unlocked threads;
+        if (!left.defined()) left = at::empty({B}, lens->options());
+        if (!ws.defined()) ws = make_bytes(*lens, need);
+        rc = p_cache_evict(&cache, (float*)wp, (const int*)tp, width, (const int*)np, (const int*)kp, recent, B, (int*)left.data_ptr(), ws.data_ptr(),
+                           (size_t)ws.numel(), s);
+    }
+    if (rc != ATTN_OK) return PyLong_FromLong(rc);
+    return out(a[6], left);
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(the addresses, in the order below; _cuda_getDevice, _cuda_getCurrentRawStream, Parameter)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     void** const to[] = {(void**)&p_fwd, (void**)&p_bwd_phases, (void**)&p_bwd_dtype, (void**)&p_bwd_bytes, (void**)&p_varlen_fwd, (void**)&p_varlen_bwd,
                          (void**)&p_varlen_bytes, (void**)&p_fwd_strided, (void**)&p_bwd_strided, (void**)&p_strided_bytes, (void**)&p_rope_fwd, (void**)&p_rope_bwd,
-                         (void**)&p_rope_bytes, (void**)&p_cache_write, (void**)&p_cache_read, (void**)&p_cache_fwd, (void**)&p_cache_bytes};
+                         (void**)&p_rope_bytes, (void**)&p_cache_write, (void**)&p_cache_read, (void**)&p_cache_fwd, (void**)&p_cache_bytes,
+                         (void**)&p_cache_chunk, (void**)&p_chunk_bytes, (void**)&p_cache_weigh, (void**)&p_cache_evict, (void**)&p_evict_bytes};
     constexpr int N = sizeof(to) / sizeof(to[0]);
     if (n != N + 3 || !PyType_Check(a[N + 2])) { PyErr_SetString(PyExc_TypeError, "bind: the addresses, two functions, a type"); return nullptr; }
     for (int i = 0; i < N; ++i) {
@@ -713,6 +822,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(fwd), METHOD(bwd), METHOD(varlen_fwd), METHOD(varlen_bwd), METHOD(fwd_strided), METHOD(bwd_strided),
                          METHOD(rope_fwd), METHOD(rope_bwd), METHOD(cache_write), METHOD(cache_read), METHOD(cache_fwd),
+                         METHOD(cache_chunk_fwd), METHOD(cache_weigh), METHOD(cache_evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -130,6 +130,43 @@ inline int64_t cache_merge_blocks(const CacheShape& s, int B, int Nq, int H, int
     return B * (((int64_t)Nq * H + per - 1) / per);
 }
 
+// ---- attention of chunks over the cache
+
+constexpr int kChunkRows = 128;         // rows (query, head of a KV head's group) of a block: 32 per wave
+
+// Keys of a tile, and blocks that a CU holds: a tile of K and V in 16 bits, twice, is 64 KiB at d = 128 and at d = 256.
+constexpr int chunk_tile_keys(int d_qk) { return d_qk <= 128 ? 64 : 32; }
+constexpr int chunk_blocks_per_cu(int d_qk) { return d_qk <= 192 ? 2 : 1; }
+
+struct ChunkShape {
+    int places;         // blocks of one round if the keys of a row tile may be divided over several, else 0
+    int min_tiles;      // of a part
+    int64_t units;      // blocks per KV head at most: (row tile, part)s
+};
+// Whether keys are divided goes by the blocks that there are for sure without: T queries in full row tiles.
+inline ChunkShape chunk_shape(int B, int T, int H, int Hkv, int d_qk)
+{
+    const int64_t G = H / Hkv, round = 256 * chunk_blocks_per_cu(d_qk);
+    const int64_t full = T * G / kChunkRows, most = full + (B < T ? B : T);
+    ChunkShape s{0, 4, most};
+    if (full * Hkv < round) {
+        s.places = (int)round;
+        s.units = round / Hkv + 2 + most;
+    }
+    return s;
+}
+
+// ---- weights of cached keys
+
+constexpr int weigh_key_blocks(int d_qk) { return d_qk <= 128 ? 2 : 1; }        // of 32 keys to a wave
+constexpr int weigh_keys(int d_qk) { return 4 * 32 * weigh_key_blocks(d_qk); }  // of a block
+inline int64_t weigh_units(int B, int Hkv, int d_qk, int64_t most) { return (int64_t)B * Hkv * ((most + weigh_keys(d_qk) - 1) / weigh_keys(d_qk)); }
+inline int weigh_blocks(int64_t units) { return (int)(units < 4096 ? units : 4096); }
+
+// ---- eviction
+
+inline int64_t evict_ints(int64_t most) { return (most + 3) / 4 * 4; }     // of a (sequence, KV head)'s list of places
+
 }  // namespace attn
 
 #if defined(__HIP__)
@@ -196,6 +233,53 @@ struct CacheFwdArgs {
 int launch_cache_fwd_bf16(const CacheFwdArgs& a);       // one object each
 int launch_cache_fwd_f16(const CacheFwdArgs& a);
 inline int launch_cache_fwd(const CacheFwdArgs& a) { return a.f16 ? launch_cache_fwd_f16(a) : launch_cache_fwd_bf16(a); }
+
+struct CacheWeighArgs {
+    CacheArgs c;
+    const void* q;
+    const float* lse;
+    float* weights;
+    Stride3 sq;
+    long long lse_batch, lse_head;
+    const int *table, *lens, *cu;       // cu null: sequence b has the queries b * Nq ... b * Nq + Nq - 1
+    int table_width;
+    int B, Nq, T, H;                    // T: rows of q in all
+    float scale;
+    int causal, fresh;
+    bool f16;
+    void* stream;
+};
+int launch_cache_weigh(const CacheWeighArgs& a);
+
+struct CacheEvictArgs {
+    CacheArgs c;
+    float* weights;
+    const int *table, *lens, *keep;
+    int* lens_out;
+    int table_width, B, recent;
+    int* places;                // [B][Hkv][evict_ints(most)]
+    void* stream;
+};
+int launch_cache_evict(const CacheEvictArgs& a);
+
+struct CacheChunkArgs {
+    CacheArgs c;
+    const void* q;              // packed [T, H, d_qk]
+    void* o;
+    float* lse;                 // [H, T]
+    long long q_row, q_head, o_row, o_head;
+    const int *table, *cu, *lens;
+    int table_width;
+    int B, T, H;
+    float scale;
+    int causal;
+    float *part_o, *part_ml;    // unnormalised results of parts: [units * Hkv][kChunkRows][d_v], and {maximum, sum} of each row
+    bool f16;
+    void* stream;
+};
+int launch_cache_chunk_bf16(const CacheChunkArgs& a);     // one object each
+int launch_cache_chunk_f16(const CacheChunkArgs& a);
+inline int launch_cache_chunk(const CacheChunkArgs& a) { return a.f16 ? launch_cache_chunk_f16(a) : launch_cache_chunk_bf16(a); }
 
 }  // namespace attn
 #endif
