@@ -800,14 +800,22 @@ int check_cache_chunk(const attn_cache_t* c, int B, int T, int H)
     if (T <= 0) return ATTN_EINVAL;
     if ((int64_t)T * H > 1 << 28 || (int64_t)T * H * (c->d_qk > c->d_v ? c->d_qk : c->d_v) > 1LL << 34) return ATTN_EUNSUPPORTED;
     const attn::ChunkShape s = attn::chunk_shape(B, T, H, c->Hkv, c->d_qk);
-    return s.units * c->Hkv > attn::kMostBlocks || (int64_t)T * H * c->d_v / 1024 >= attn::kMostBlocks ? ATTN_EUNSUPPORTED : ATTN_OK;
+    if (s.units * c->Hkv > attn::kMostBlocks) return ATTN_EUNSUPPORTED;
+    const int per = 256 / (c->d_v / 4);
+    return s.places && (int64_t)T * ((H + per - 1) / per) > attn::kMostBlocks ? ATTN_EUNSUPPORTED : ATTN_OK;
 }
 
-// partial results of every block, if there may be more than one to a row tile: O | maximum and sum
-size_t chunk_part_rows(const attn_cache_t* c, int B, int T, int H)
+// partial results of every block, if there may be more than one to a row tile: O | maximum and sum | where a sequence's parts are
+CacheParts chunk_parts(const attn_cache_t* c, int B, int T, int H)
 {
     const attn::ChunkShape s = attn::chunk_shape(B, T, H, c->Hkv, c->d_qk);
-    return s.places == 0 ? 0 : (size_t)s.units * c->Hkv * attn::kChunkRows;
+    if (s.places == 0) return {0, 0, 256};
+    const size_t rows = (size_t)s.units * (size_t)c->Hkv * attn::kChunkRows;
+    CacheParts w;
+    w.ml_off = align_up(rows * c->d_v * sizeof(float), 256);
+    w.merge_off = w.ml_off + align_up(rows * 2 * sizeof(float), 256);
+    w.total = w.merge_off + align_up((size_t)B * 4 * sizeof(int), 256);
+    return w;
 }
 
 }  // namespace
@@ -815,8 +823,7 @@ size_t chunk_part_rows(const attn_cache_t* c, int B, int T, int H)
 size_t attn_cache_chunk_workspace_bytes(const attn_cache_t* cache, int B, int T, int H)
 {
     if (check_cache_chunk(cache, B, T, H) != ATTN_OK) return 0;
-    const size_t rows = chunk_part_rows(cache, B, T, H);
-    return rows == 0 ? 256 : rows * (cache->d_v + 2) * sizeof(float);
+    return chunk_parts(cache, B, T, H).total;
 }
 
 int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, void* o, const attn_strides_t* so, float* lse,
@@ -832,7 +839,8 @@ int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, co
     if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4) || misaligned(block_table, 4) || misaligned(cu_seqlens, 4) || misaligned(lens, 4) ||
         misaligned(workspace, 256))
         return ATTN_EINVAL;
-    if (workspace_bytes < attn_cache_chunk_workspace_bytes(cache, B, T, H)) return ATTN_EINVAL;
+    const CacheParts w = chunk_parts(cache, B, T, H);
+    if (workspace_bytes < w.total) return ATTN_EINVAL;
     attn::CacheChunkArgs a = {};
     a.c = cache_args(cache);
     a.q = q;
@@ -851,8 +859,10 @@ int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, co
     a.H = H;
     a.scale = scale;
     a.causal = causal != 0;
-    a.part_o = static_cast<float*>(workspace);
-    a.part_ml = a.part_o + chunk_part_rows(cache, B, T, H) * cache->d_v;
+    char* ws = static_cast<char*>(workspace);
+    a.part_o = reinterpret_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float*>(ws + w.ml_off);
+    a.merge = reinterpret_cast<int*>(ws + w.merge_off);
     a.f16 = dtype == ATTN_F16;
     a.stream = stream;
     const int rc = attn::launch_cache_chunk(a);

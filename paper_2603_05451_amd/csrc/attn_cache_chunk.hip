@@ -32,7 +32,8 @@ struct ChunkWork {
     ChunkSeq held;
     int part_tiles;
 
-    __device__ __forceinline__ ChunkSeq fetch(int b) const
+    __device__ __forceinline__ ChunkSeq fetch(int b) const { return fetch(p, cu, lens, b); }
+    __device__ __forceinline__ static ChunkSeq fetch(const ChunkPlanArgs& p, const int* __restrict__ cu, const int* __restrict__ lens, int b)
     {
         if (b >= p.B) return {0, 0, 0};
         const int q0 = cu[b], q1 = cu[b + 1];
@@ -108,30 +109,21 @@ struct ChunkWork {
         at.rt = rts - 1 - (local - at.part * rts);
         at.part_tiles = (tiles + at.parts - 1) / at.parts;
     }
-    // The sequence of query t, and the unit of the first part of the row tile of its row `row_in_query` (with all its parts a `stride` apart).
-    __device__ __forceinline__ bool find_query(int t, int row_in_query, ChunkPlace& at, int& row, int& stride) const
+    // The sequence of query t, as its lengths say (what its parts are, the attention kernel has left behind).
+    __device__ __forceinline__ static bool of_query(const ChunkPlanArgs& p, const int* __restrict__ cu, const int* __restrict__ lens, int t, ChunkSeq& s, int& b)
     {
-        bool found = false;
-        int before = 0;
-        each([&](const ChunkSeq& s, int) {
-            const int mine = units(s), upto = before + wave_prefix(mine);
-            const uint64_t here = __ballot(s.nq > 0 && t >= s.q0 && t < s.q0 + s.nq);
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            const ChunkSeq x = fetch(p, cu, lens, b0 + (threadIdx.x & 63));
+            const uint64_t here = __ballot(x.nq > 0 && t >= x.q0 && t < x.q0 + x.nq);
             if (here) {
                 const int l = __builtin_ctzll(here);
-                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-                at.s = {of(s.q0), of(s.nq), of(s.len)};
-                row = (t - at.s.q0) * p.G + row_in_query;
-                at.rt = row / kChunkRows;
-                at.parts = parts(at.s);
-                at.part_tiles = (key_tiles(at.s) + at.parts - 1) / at.parts;
-                stride = row_tiles(at.s);
-                at.unit = of(upto) - of(mine) + stride - 1 - at.rt;
-                return found = true;
+                auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+                s = {of(x.q0), of(x.nq), of(x.len)};
+                b = b0 + l;
+                return true;
             }
-            before = __builtin_amdgcn_readlane(upto, 63);
-            return false;
-        });
-        return found;
+        }
+        return false;
     }
 };
 

@@ -274,6 +274,7 @@ struct CacheChunkArgs {
     float scale;
     int causal;
     float *part_o, *part_ml;    // unnormalised results of parts: [units * Hkv][kChunkRows][d_v], and {maximum, sum} of each row
+    int* merge;                 // [B][4]: where a sequence's parts are
     bool f16;
     void* stream;
 };
