@@ -358,7 +358,7 @@ int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const at
  *     B is 65536 at most, T * H * d up to 2^34, T * H up to 2^28.
  *   workspace: attn_cache_chunk_workspace_bytes(...) bytes, 256-byte aligned, contents ignored.  One kernel, and a merge where there are so few rows
  *   that keys may be divided over blocks (without which the o and lse of divided sequences are untouched). */
-size_t attn_cache_chunk_workspace_bytes(const attn_cache_t* cache, int B, int T, int H);
+size_t attn_cache_chunk_workspace_bytes(const attn_cache_t* cache, int B, int T, int H, int table_width);
 int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, void* o, const attn_strides_t* so, float* lse,
                          const int* block_table, int table_width, const int* cu_seqlens, const int* lens, int B, int T, int H, float scale, int causal,
                          void* workspace, size_t workspace_bytes, void* stream);

@@ -99,7 +99,7 @@ def lib():
         L.attn_cache_workspace_bytes.restype = sz
         L.attn_cache_fwd.argtypes = [i, cp, vp, sp, vp, sp, vp, vp, i, vp, i, i, i, f, i, vp, sz, vp]
         L.attn_cache_fwd.restype = i
-        L.attn_cache_chunk_workspace_bytes.argtypes = [cp, i, i, i]
+        L.attn_cache_chunk_workspace_bytes.argtypes = [cp, i, i, i, i]
         L.attn_cache_chunk_workspace_bytes.restype = sz
         L.attn_cache_chunk_fwd.argtypes = [i, cp, vp, sp, vp, sp, vp, vp, i, vp, vp, i, i, i, f, i, vp, sz, vp]
         L.attn_cache_chunk_fwd.restype = i
@@ -759,8 +759,8 @@ def attn_cache_fwd(q, cache, block_table, lens, scale, causal, o=None, lse=None,
     return o, lse
 
 
-def attn_cache_chunk_workspace_bytes(cache, B, T, H) -> int:
-    return int(lib().attn_cache_chunk_workspace_bytes(ctypes.byref(_cache(cache, None)), B, T, H))
+def attn_cache_chunk_workspace_bytes(cache, B, T, H, table_width) -> int:
+    return int(lib().attn_cache_chunk_workspace_bytes(ctypes.byref(_cache(cache, None)), B, T, H, table_width))
 
 
 def attn_cache_chunk_fwd(q, cache, block_table, cu_seqlens, lens, scale, causal, o=None, lse=None, workspace=None, stream=None):
@@ -790,7 +790,7 @@ def attn_cache_chunk_fwd(q, cache, block_table, cu_seqlens, lens, scale, causal,
     _here(lse, "lse", torch.float32, stream)
     lse_p = _dev_lse(lse, (H, T), "H,T")
     if workspace is None:
-        workspace = _empty((max(lib().attn_cache_chunk_workspace_bytes(ctypes.byref(layout), B, T, H), 256),), torch.uint8, q.device, stream)
+        workspace = _empty((max(lib().attn_cache_chunk_workspace_bytes(ctypes.byref(layout), B, T, H, width), 256),), torch.uint8, q.device, stream)
     else:
         _scratch(workspace, stream)
     _check(lib().attn_cache_chunk_fwd(code, ctypes.byref(layout), x.data_ptr(), _strides(x), y.data_ptr(), _strides(y), lse_p, table, width, cu, keys,

@@ -794,21 +794,21 @@ int check_cache_table(const attn_cache_t* c, int B, int H, int table_width)
     return most > 0x7fffffffLL - 1024 || B > 65536 ? ATTN_EUNSUPPORTED : ATTN_OK;
 }
 
-int check_cache_chunk(const attn_cache_t* c, int B, int T, int H)
+int check_cache_chunk(const attn_cache_t* c, int B, int T, int H, int table_width)
 {
-    if (int rc = check_cache_table(c, B, H, 1)) return rc;
+    if (int rc = check_cache_table(c, B, H, table_width)) return rc;
     if (T <= 0) return ATTN_EINVAL;
     if ((int64_t)T * H > 1 << 28 || (int64_t)T * H * (c->d_qk > c->d_v ? c->d_qk : c->d_v) > 1LL << 34) return ATTN_EUNSUPPORTED;
-    const attn::ChunkShape s = attn::chunk_shape(B, T, H, c->Hkv, c->d_qk);
+    const attn::ChunkShape s = attn::chunk_shape(B, T, H, c->Hkv, c->d_qk, (int64_t)table_width * c->page);
     if (s.units * c->Hkv > attn::kMostBlocks) return ATTN_EUNSUPPORTED;
     const int per = 256 / (c->d_v / 4);
     return s.places && (int64_t)T * ((H + per - 1) / per) > attn::kMostBlocks ? ATTN_EUNSUPPORTED : ATTN_OK;
 }
 
 // partial results of every block, if there may be more than one to a row tile: O | maximum and sum | where a sequence's parts are
-CacheParts chunk_parts(const attn_cache_t* c, int B, int T, int H)
+CacheParts chunk_parts(const attn_cache_t* c, int B, int T, int H, int table_width)
 {
-    const attn::ChunkShape s = attn::chunk_shape(B, T, H, c->Hkv, c->d_qk);
+    const attn::ChunkShape s = attn::chunk_shape(B, T, H, c->Hkv, c->d_qk, (int64_t)table_width * c->page);
     if (s.places == 0) return {0, 0, 256};
     const size_t rows = (size_t)s.units * (size_t)c->Hkv * attn::kChunkRows;
     CacheParts w;
@@ -820,10 +820,10 @@ CacheParts chunk_parts(const attn_cache_t* c, int B, int T, int H)
 
 }  // namespace
 
-size_t attn_cache_chunk_workspace_bytes(const attn_cache_t* cache, int B, int T, int H)
+size_t attn_cache_chunk_workspace_bytes(const attn_cache_t* cache, int B, int T, int H, int table_width)
 {
-    if (check_cache_chunk(cache, B, T, H) != ATTN_OK) return 0;
-    return chunk_parts(cache, B, T, H).total;
+    if (check_cache_chunk(cache, B, T, H, table_width) != ATTN_OK) return 0;
+    return chunk_parts(cache, B, T, H, table_width).total;
 }
 
 int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, void* o, const attn_strides_t* so, float* lse,
@@ -832,14 +832,13 @@ int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, co
 {
     if (dtype != ATTN_BF16 && dtype != ATTN_F16) return ATTN_EUNSUPPORTED;
     if (!q || !o || !lse || !block_table || !cu_seqlens || !lens || !workspace) return ATTN_EINVAL;
-    if (int rc = check_cache_table(cache, B, H, table_width)) return rc;
-    if (int rc = check_cache_chunk(cache, B, T, H)) return rc;
+    if (int rc = check_cache_chunk(cache, B, T, H, table_width)) return rc;
     if (bad_view(sq, 1, T, H) || bad_view(so, 1, T, H)) return ATTN_EINVAL;
     if (!(scale > 0.0f) || !(scale < 1e30f)) return ATTN_EINVAL;
     if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4) || misaligned(block_table, 4) || misaligned(cu_seqlens, 4) || misaligned(lens, 4) ||
         misaligned(workspace, 256))
         return ATTN_EINVAL;
-    const CacheParts w = chunk_parts(cache, B, T, H);
+    const CacheParts w = chunk_parts(cache, B, T, H, table_width);
     if (workspace_bytes < w.total) return ATTN_EINVAL;
     attn::CacheChunkArgs a = {};
     a.c = cache_args(cache);

@@ -12,7 +12,7 @@ namespace {
 // ---- which rows and keys a block takes, from the boundaries and lengths in device memory
 struct ChunkPlanArgs {
     int B, T, G, Hkv, page_shift, most;     // most: keys that a row of the table has room for
-    int tile_keys, places, min_tiles;       // chunk_shape's; places = 0: no sequence's keys are divided
+    int tile_keys, places;                  // keys of a step of the kernel for many rows; chunk_shape's places (0: no sequence's keys are divided)
 };
 // A sequence: its first query, number of queries (0: there is nothing to do) and of keys.
 struct ChunkSeq {
@@ -21,8 +21,11 @@ struct ChunkSeq {
 struct ChunkPlace {
     ChunkSeq s;
     int b;                                  // its index
-    int rt, part, parts, part_tiles, unit;  // row tile; which of the parts of its keys, of so many key tiles; index of that part's unit
+    int rt, part, parts, part_steps, unit;  // row tile; which of the parts of its keys, of so many steps; index of that part's unit
 };
+// Sequences with few rows (queries times heads of a group) go by another body: 32 rows to a block, 128 keys to a step of it.
+__device__ __forceinline__ bool chunk_few(const ChunkSeq& s, int G) { return s.nq * G <= kChunkFew; }
+__device__ __forceinline__ int chunk_rows(const ChunkSeq& s, int G) { return chunk_few(s, G) ? 32 : kChunkRows; }
 
 // What every wave of a launch finds out, a sequence per lane (the first 64 stay in registers).
 struct ChunkWork {
@@ -30,7 +33,7 @@ struct ChunkWork {
     const int* __restrict__ cu;
     const int* __restrict__ lens;
     ChunkSeq held;
-    int part_tiles;
+    int cost;               // of a part, in quarters of a step
 
     __device__ __forceinline__ ChunkSeq fetch(int b) const { return fetch(p, cu, lens, b); }
     __device__ __forceinline__ static ChunkSeq fetch(const ChunkPlanArgs& p, const int* __restrict__ cu, const int* __restrict__ lens, int b)
@@ -49,32 +52,36 @@ struct ChunkWork {
         for (int b0 = 64; b0 < p.B; b0 += 64)
             if (f(fetch(b0 + lane), b0 + lane)) return;
     }
-    __device__ __forceinline__ int row_tiles(const ChunkSeq& s) const { return (s.nq * p.G + kChunkRows - 1) / kChunkRows; }
-    __device__ __forceinline__ int key_tiles(const ChunkSeq& s) const { return (s.len + p.tile_keys - 1) / p.tile_keys; }
+    __device__ __forceinline__ int row_tiles(const ChunkSeq& s) const { const int n = chunk_rows(s, p.G); return (s.nq * p.G + n - 1) / n; }
+    __device__ __forceinline__ int step_keys(const ChunkSeq& s) const { return chunk_few(s, p.G) ? 128 : p.tile_keys; }
+    __device__ __forceinline__ int steps(const ChunkSeq& s) const { const int n = step_keys(s); return (s.len + n - 1) / n; }
+    __device__ __forceinline__ int step_cost(const ChunkSeq& s) const { return chunk_few(s, p.G) ? kChunkFewCost : 4; }
     __device__ __forceinline__ int parts(const ChunkSeq& s) const
     {
-        return p.places == 0 ? 1 : max(1, (key_tiles(s) + part_tiles - 1) / part_tiles);
+        if (p.places == 0) return 1;
+        const int each = max(4, (cost + step_cost(s) - 1) / step_cost(s));     // a part has four steps or more
+        return max(1, (steps(s) + each - 1) / each);
     }
     __device__ __forceinline__ int units(const ChunkSeq& s) const { return row_tiles(s) * parts(s); }
 
-    // Key tiles of a part: all key tiles of all row tiles in about `places` parts (a round of blocks), longer if the sequences' last,
-    // shorter parts would make it more.
+    // What a part costs: all steps of all row tiles in about `places` parts (a round of blocks), longer if the sequences' last, shorter parts
+    // would make it more.
     __device__ __forceinline__ ChunkWork(const ChunkPlanArgs& plan, const int* __restrict__ c, const int* __restrict__ l) : p(plan), cu(c), lens(l)
     {
         held = fetch(threadIdx.x & 63);
-        part_tiles = 1;
+        cost = 1;
         if (p.places == 0) return;
         float total = 0.f;
-        each([&](const ChunkSeq& s, int) { total += (float)row_tiles(s) * (float)key_tiles(s); return false; });
+        each([&](const ChunkSeq& s, int) { total += (float)row_tiles(s) * (float)steps(s) * (float)step_cost(s); return false; });
         total = wave_sum(total);
         const int places = max(1, p.places / p.Hkv);
-        part_tiles = max(p.min_tiles, (int)ceilf(total / (float)places));
+        cost = (int)fminf(ceilf(total / (float)places), 1e9f);
         for (int i = 0; i < 3; ++i) {
             int n = 0;
             each([&](const ChunkSeq& s, int) { n += units(s); return false; });
             n = wave_sum(n);
             if (n <= places) break;
-            part_tiles += max(1, part_tiles / 4);
+            cost += cost / 4 + 1;
         }
     }
     // The sequence and its part that unit u is; false behind the last one.
@@ -103,11 +110,11 @@ struct ChunkWork {
     // mask, to the first.
     __device__ __forceinline__ void place(ChunkPlace& at, int local) const
     {
-        const int rts = row_tiles(at.s), tiles = key_tiles(at.s);
+        const int rts = row_tiles(at.s), n = steps(at.s);
         at.parts = parts(at.s);
         at.part = local / rts;
         at.rt = rts - 1 - (local - at.part * rts);
-        at.part_tiles = (tiles + at.parts - 1) / at.parts;
+        at.part_steps = (n + at.parts - 1) / at.parts;
     }
     // The sequence of query t, as its lengths say (what its parts are, the attention kernel has left behind).
     __device__ __forceinline__ static bool of_query(const ChunkPlanArgs& p, const int* __restrict__ cu, const int* __restrict__ lens, int t, ChunkSeq& s, int& b)

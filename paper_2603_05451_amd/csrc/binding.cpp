@@ -718,7 +718,7 @@ PyObject* cache_chunk_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (a[9] != Py_None) { const at::Tensor* t = c.tensor(a[9]); if (t) { ws = *t; if (t->scalar_type() != at::kByte || !t->is_contiguous()) c.ok = false; } }
     if (o.defined()) { c.rows(&o, c.type, os); --c.nstrides; }
     if (!c.ok) NOT_HERE;
-    const size_t need = ws.defined() ? 0 : p_chunk_bytes(&cache, B, T, H);
+    const size_t need = ws.defined() ? 0 : p_chunk_bytes(&cache, B, T, H, width);
     void* s = c.stream_here(a[10]);
     if (!c.ok) NOT_HERE;
     int rc;

@@ -133,6 +133,8 @@ inline int64_t cache_merge_blocks(const CacheShape& s, int B, int Nq, int H, int
 // ---- attention of chunks over the cache
 
 constexpr int kChunkRows = 128;         // rows (query, head of a KV head's group) of a block: 32 per wave
+constexpr int kChunkFew = 64;           // a sequence with no more rows goes by the body for few: 32 rows of a block, whose waves share the keys
+constexpr int kChunkFewCost = 2;        // a step of that body (128 keys), in quarters of a step of the other
 
 // Keys of a tile, and blocks that a CU holds: a tile of K and V in 16 bits, twice, is 64 KiB at d = 128 and at d = 256.
 constexpr int chunk_tile_keys(int d_qk) { return d_qk <= 128 ? 64 : 32; }
@@ -140,18 +142,17 @@ constexpr int chunk_blocks_per_cu(int d_qk) { return d_qk <= 192 ? 2 : 1; }
 
 struct ChunkShape {
     int places;         // blocks of one round if the keys of a row tile may be divided over several, else 0
-    int min_tiles;      // of a part
     int64_t units;      // blocks per KV head at most: (row tile, part)s
 };
-// Whether keys are divided goes by the blocks that there are for sure without: T queries in full row tiles.
-inline ChunkShape chunk_shape(int B, int T, int H, int Hkv, int d_qk)
+// Whether keys are divided goes by the blocks that there are for sure without (T queries in full row tiles), and by the table's width.
+inline ChunkShape chunk_shape(int B, int T, int H, int Hkv, int d_qk, int64_t most)
 {
     const int64_t G = H / Hkv, round = 256 * chunk_blocks_per_cu(d_qk);
-    const int64_t full = T * G / kChunkRows, most = full + (B < T ? B : T);
-    ChunkShape s{0, 4, most};
-    if (full * Hkv < round) {
+    const int64_t full = T * G / kChunkRows, units = full + 2 * (int64_t)(B < T ? B : T);
+    ChunkShape s{0, units};
+    if (full * Hkv < round && most > (T * G > (int64_t)kChunkFew * B ? 512 : 1536)) {
         s.places = (int)round;
-        s.units = round / Hkv + 2 + most;
+        s.units = round / Hkv + 2 + units;
     }
     return s;
 }

@@ -56,7 +56,7 @@ def test_undivided(dqk, dv, Hkv, G, seqs):
     import paper_2603_05451_amd as A
     q, cache, t, cu, lens = _case(3, seqs, Hkv, G, dqk, dv, 4, 64, BF)
     c = cref.on_gpu(cache)
-    assert A.attn_cache_chunk_workspace_bytes(c, len(seqs), q.shape[0], Hkv * G) == 256
+    assert A.attn_cache_chunk_workspace_bytes(c, len(seqs), q.shape[0], Hkv * G, t.shape[1]) == 256
     o, lse = _run(q, c, t, cu, lens, dqk ** -0.5, True)
     cref.check_attention(q, cache, t, cu, lens, dqk ** -0.5, True, o.cpu(), lse.cpu(), 4)
 
@@ -101,7 +101,7 @@ def test_views_padding_and_given_outputs():
     o = torch.full((4, T, 128), 7.0, dtype=BF, device="cuda").transpose(0, 1)
     lse = torch.full((4, T), 7.0, device="cuda")
     c = cref.on_gpu(cache)
-    ws = torch.empty(A.attn_cache_chunk_workspace_bytes(c, 2, T, 4), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(A.attn_cache_chunk_workspace_bytes(c, 2, T, 4, t.shape[1]), dtype=torch.uint8, device="cuda")
     r = A.attn_cache_chunk_fwd(wide[:, 2:6, :128], c, t.cuda(), cu.cuda(), lens.cuda(), 0.1, True, o=o, lse=lse, workspace=ws)
     assert r[0] is o and r[1] is lse
     cref.check_attention(q, cache, t, cu, lens, 0.1, True, o.cpu(), lse.cpu(), 8)
@@ -208,7 +208,7 @@ def test_again_on_a_stream_and_in_a_graph():
     state = {"q": torch.zeros(T, 4, 128, dtype=BF, device="cuda"), "t": torch.zeros(3, width, dtype=torch.int32, device="cuda"),
              "cu": torch.zeros(4, dtype=torch.int32, device="cuda"), "lens": torch.zeros(3, dtype=torch.int32, device="cuda"),
              "o": torch.zeros(T, 4, 128, dtype=BF, device="cuda"), "lse": torch.zeros(4, T, device="cuda")}
-    ws = torch.empty(A.attn_cache_chunk_workspace_bytes(c, 3, T, 4), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(A.attn_cache_chunk_workspace_bytes(c, 3, T, 4, width), dtype=torch.uint8, device="cuda")
 
     def put(x):
         state["q"].zero_()
