@@ -910,7 +910,9 @@ int attn_cache_weigh(int dtype, const attn_cache_t* cache, const void* q, const 
 
 size_t attn_cache_evict_workspace_bytes(const attn_cache_t* cache, int B, int table_width)
 {
-    if (check_cache_table(cache, B, cache ? cache->Hkv : 0, table_width) != ATTN_OK || (int64_t)B * cache->Hkv > attn::kMostBlocks) return 0;
+    if (check_cache_table(cache, B, cache ? cache->Hkv : 0, table_width) != ATTN_OK || (int64_t)B * cache->Hkv > attn::kMostBlocks ||
+        (int64_t)table_width * cache->page > 1 << 26)
+        return 0;
     return align_up((size_t)B * (size_t)cache->Hkv * (size_t)attn::evict_ints((int64_t)table_width * cache->page) * sizeof(int), 256);
 }
 
@@ -920,7 +922,8 @@ int attn_cache_evict(const attn_cache_t* cache, float* weights, const int* block
     if (!weights || !block_table || !lens || !keep || !lens_out || !workspace) return ATTN_EINVAL;
     if (int rc = check_cache_table(cache, B, cache ? cache->Hkv : 0, table_width)) return rc;
     if (recent < 0 || lens_out == lens || lens_out == keep) return ATTN_EINVAL;
-    if ((int64_t)B * cache->Hkv > attn::kMostBlocks) return ATTN_EUNSUPPORTED;
+    if ((int64_t)B * cache->Hkv > attn::kMostBlocks || (int64_t)table_width * cache->page > 1 << 26) return ATTN_EUNSUPPORTED;
+    if (misaligned(cache->k_scale, 8) || misaligned(cache->v_scale, 8)) return ATTN_EINVAL;
     if (misaligned(weights, 16) || misaligned(block_table, 4) || misaligned(lens, 4) || misaligned(keep, 4) || misaligned(lens_out, 4) || misaligned(workspace, 256))
         return ATTN_EINVAL;
     if (workspace_bytes < attn_cache_evict_workspace_bytes(cache, B, table_width)) return ATTN_EINVAL;
@@ -936,7 +939,8 @@ int attn_cache_evict(const attn_cache_t* cache, float* weights, const int* block
     a.recent = recent;
     a.places = static_cast<int*>(workspace);
     a.stream = stream;
-    return attn::launch_cache_evict(a) == 0 ? ATTN_OK : ATTN_ELAUNCH;
+    const int rc = attn::launch_cache_evict(a);
+    return rc == 0 ? ATTN_OK : (rc == -2 ? ATTN_EUNSUPPORTED : ATTN_ELAUNCH);
 }
 
 const char* attn_strerror(int code)

@@ -18,11 +18,13 @@ namespace {
 
 struct EvictPlan {
     int Hkv, page_shift, most, table_width, pages, recent;
-    int kb, vb, ksb, vsb;       // bytes of a row: codes and scales of keys and values
     int64_t ints;
 };
 
 constexpr int kThreads = 1024;
+constexpr int kHeld = 8;            // turns of 4 keys to a thread whose weights stay in registers: 32 768 keys
+constexpr int kListed = 8192;       // holes and movers that LDS has room for (else they go to the workspace)
+constexpr int kAtOnce = 4;          // pieces of rows that a thread moves in a turn
 
 // Weights in ascending order as whole numbers: 0 is a row that is not in the cache, NaN the greatest, -0 and 0 are equal.
 __device__ __forceinline__ uint32_t least_first(float w)
@@ -46,17 +48,42 @@ __device__ __forceinline__ void block_sums(int x, ATTN_LDS int* part, int& befor
     __syncthreads();
 }
 
+// The scale bytes of a row: BYTES of them, in words as large as their alignment is for certain.
+template <int BYTES>
+struct ScaleRow {
+    using Word = std::conditional_t<BYTES % 8 == 0, uint64_t, std::conditional_t<BYTES % 4 == 0, uint32_t, std::conditional_t<BYTES % 2 == 0, uint16_t, uint8_t>>>;
+    static constexpr int N = BYTES / sizeof(Word);
+    Word w[N];
+    __device__ __forceinline__ void fill(uint8_t byte)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = (Word)(0x0101010101010101ull * byte);
+    }
+    __device__ __forceinline__ void load(const uint8_t* all, int64_t row)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = ((const Word*)all)[row * N + i];
+    }
+    __device__ __forceinline__ void store(uint8_t* all, int64_t row) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) ((Word*)all)[row * N + i] = w[i];
+    }
+};
+
+template <int DQK, int DV, int BITS>
 __global__ void __launch_bounds__(kThreads)
 attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint8_t* __restrict__ vc, uint8_t* __restrict__ vs,
                         float* __restrict__ weights, const int* __restrict__ table, const int* __restrict__ lens, const int* __restrict__ keep,
                         int* __restrict__ lens_out, EvictPlan plan, int* __restrict__ places_of_all)
 {
+    constexpr int KROW = DQK * BITS / 8, VROW = DV * BITS / 8;
     __shared__ int count[2048];
     __shared__ int part_[32];
     __shared__ int found[2];
+    __shared__ int list[kListed];
     ATTN_LDS int* const part = (ATTN_LDS int*)part_;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x;
     const int b = (int)blockIdx.x / plan.Hkv, kvh = (int)blockIdx.x - b * plan.Hkv;
     const int len = min(max(lens[b], 0), plan.most), left = min(len, max(keep[b], 0));
     if (kvh == 0 && tid == 0) lens_out[b] = left;
@@ -78,26 +105,50 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
         for (int e = 0; e < 4; ++e) x[e] = r >= 0 ? least_first(w[e]) : 0u;
     };
     int* const places = places_of_all + (int64_t)blockIdx.x * plan.ints;
+    const bool in_lds = 2 * min(stay, len - left) <= kListed;          // (there are no more holes than rows that leave, nor than that stay)
 
     int moves = 0;
     if (stay > 0) {
+        uint32_t held[kHeld][4];
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (4 * kThreads * i < of) keys_at(min(4 * (kThreads * i + tid), of - 1) & ~3, held[i]);
+        // f(first of 4 keys, their numbers) for every turn of the block
+        auto each = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (4 * kThreads * i < of) f(4 * (kThreads * i + tid), held[i]);
+#pragma unroll 1
+            for (int j0 = 4 * kThreads * kHeld; j0 < of; j0 += 4 * kThreads) {
+                const int j = j0 + 4 * tid;
+                uint32_t x[4] = {0, 0, 0, 0};
+                if (j < of) keys_at(j, x);
+                f(j, x);
+            }
+        };
+
         // ---- the stay-th greatest: its digits from the highest on
         uint32_t prefix = 0;                               // those found so far
         int wanted = stay;                                 // the greatest `wanted` of the keys that begin with them
-#pragma unroll 1
+#pragma unroll
         for (int digit = 0; digit < 3; ++digit) {
-            const int low = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
-            for (int i = tid; i < 2048; i += kThreads) count[i] = 0;
+            constexpr int low_of[] = {21, 10, 0};
+            const int low = low_of[digit], bits = digit == 2 ? 10 : 11;
+            count[tid] = count[tid + kThreads] = 0;
             __syncthreads();
-            for (int j = 4 * tid; j < of; j += 4 * kThreads) {
-                uint32_t x[4];
-                keys_at(j, x);
+            each([&](int j, const uint32_t (&x)[4]) __attribute__((always_inline)) {
+                int at[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) at[e] = j + e < of && (digit == 0 || x[e] >> (low + bits) == prefix) ? (int)((x[e] >> low) & ((1u << bits) - 1)) : -1;
+                // (equal ones in one go: lanes that add to one place do so one after the other)
+                int n = 1;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const bool mine = j + e < of && (digit == 0 || x[e] >> (low + bits) == prefix);
-                    if (mine) atomicAdd(&count[(x[e] >> low) & ((1 << bits) - 1)], 1);
+                    const bool more = e < 3 && at[e] == at[e < 3 ? e + 1 : 3];
+                    if (!more && at[e] >= 0) atomicAdd(&count[at[e]], n);
+                    n = more ? n + 1 : 1;
                 }
-            }
+            });
             __syncthreads();
             // places 2 tid and 2 tid + 1, counted from the greatest
             const int hi = count[2047 - 2 * tid], lo = count[2046 - 2 * tid];
@@ -111,16 +162,12 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
             __syncthreads();
             prefix = prefix << bits | (uint32_t)found[0];
             wanted = found[1];
-            __syncthreads();
         }
         const uint32_t least = prefix;                     // of the survivors; `wanted` of those that are equal to it survive, the first ones
 
         // ---- holes and movers, in ascending order
         int equal = 0;
-        for (int j0 = 0; j0 < of; j0 += 4 * kThreads) {
-            const int j = j0 + 4 * tid;
-            uint32_t x[4] = {0, 0, 0, 0};
-            if (j < of) keys_at(j, x);
+        each([&](int j, const uint32_t (&x)[4]) __attribute__((always_inline)) {
             int n = 0, before, all;
 #pragma unroll
             for (int e = 0; e < 4; ++e) n += j + e < of && x[e] == least;
@@ -142,68 +189,97 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
             moves += all;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (listed[e]) places[before++] = j + e;
-        }
+                if (listed[e]) {
+                    if (in_lds) list[before] = j + e;
+                    else places[before] = j + e;
+                    ++before;
+                }
+        });
         moves /= 2;
+        __syncthreads();
     }
-    __syncthreads();
 
-    // ---- rows from `from` to `to`, both of this sequence and head
-    // a piece of `bytes` of a row: 16 codes' bytes, all scales, or the weight
-    const int kp = plan.kb / 16, vp = plan.vb / 16, pieces = kp + vp + 1;
+    // ---- movers into holes, then the recent rows.  A turn reads all it moves before it writes.  What it writes is read by no later turn: holes are
+    // read by none, and a recent row's new place lies below those that later ones come from.
+    constexpr int KP = KROW / 16, VP = VROW / 16, PIECES = KP + VP + 1;            // of a row: 16 bytes of codes, and all scales and the weight
     struct Piece {
-        u32x4 w;
-        uint64_t k_scale, v_scale;
-        float weight;
+        union {
+            u32x4 w;
+            struct {
+                ScaleRow<DQK / 32> k_scale;
+                ScaleRow<DV / 32> v_scale;
+                float weight;
+            } s;
+        };
+        __device__ Piece() {}
     };
-    auto load = [&](Piece& x, int64_t r, int piece) __attribute__((always_inline)) {
-        if (piece < kp) x.w = r < 0 ? u32x4{0, 0, 0, 0} : *(const u32x4*)(kc + r * plan.kb + 16 * piece);
-        else if (piece < kp + vp) x.w = r < 0 ? u32x4{0, 0, 0, 0} : *(const u32x4*)(vc + r * plan.vb + 16 * (piece - kp));
-        else {
-            x.k_scale = x.v_scale = r < 0 ? ~0ull : 0ull;              // (a row of a page that is not there is NaN)
-            for (int i = 0; r >= 0 && i < plan.ksb; ++i) x.k_scale |= (uint64_t)ks[r * plan.ksb + i] << (8 * i);
-            for (int i = 0; r >= 0 && i < plan.vsb; ++i) x.v_scale |= (uint64_t)vs[r * plan.vsb + i] << (8 * i);
-            x.weight = r < 0 ? 0.f : weights[r];
+    const uint32_t items = (uint32_t)(moves + recent) * PIECES;        // (2^26 * 33 at most)
+    for (uint32_t i0 = 0; i0 < items; i0 += kAtOnce * kThreads) {
+        Piece x[kAtOnce];
+        int64_t to[kAtOnce];
+        int piece[kAtOnce];
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+            const uint32_t i = i0 + kThreads * e + tid;
+            to[e] = -1;
+            if (i >= items) continue;
+            const int m = (int)(i / PIECES);
+            piece[e] = (int)(i % PIECES);
+            auto place = [&](int n) __attribute__((always_inline)) { return in_lds ? list[n] : places[n]; };
+            const int64_t r = row_of(m < moves ? place(moves + m) : of + m - moves);
+            to[e] = row_of(m < moves ? place(m) : stay + m - moves);
+            // (a row of a page that is not there is NaN, its weight 0)
+            if (piece[e] < KP) x[e].w = r < 0 ? u32x4{0, 0, 0, 0} : *(const u32x4*)(kc + r * KROW + 16 * piece[e]);
+            else if (piece[e] < KP + VP) x[e].w = r < 0 ? u32x4{0, 0, 0, 0} : *(const u32x4*)(vc + r * VROW + 16 * (piece[e] - KP));
+            else if (r < 0) {
+                x[e].s.k_scale.fill(255);
+                x[e].s.v_scale.fill(255);
+                x[e].s.weight = 0.f;
+            } else {
+                x[e].s.k_scale.load(ks, r);
+                x[e].s.v_scale.load(vs, r);
+                x[e].s.weight = weights[r];
+            }
         }
-    };
-    auto store = [&](const Piece& x, int64_t r, int piece) __attribute__((always_inline)) {
-        if (r < 0) return;
-        if (piece < kp) *(u32x4*)(kc + r * plan.kb + 16 * piece) = x.w;
-        else if (piece < kp + vp) *(u32x4*)(vc + r * plan.vb + 16 * (piece - kp)) = x.w;
-        else {
-            for (int i = 0; i < plan.ksb; ++i) ks[r * plan.ksb + i] = (uint8_t)(x.k_scale >> (8 * i));
-            for (int i = 0; i < plan.vsb; ++i) vs[r * plan.vsb + i] = (uint8_t)(x.v_scale >> (8 * i));
-            weights[r] = x.weight;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+            const int64_t r = to[e];
+            if (r < 0) continue;
+            if (piece[e] < KP) *(u32x4*)(kc + r * KROW + 16 * piece[e]) = x[e].w;
+            else if (piece[e] < KP + VP) *(u32x4*)(vc + r * VROW + 16 * (piece[e] - KP)) = x[e].w;
+            else {
+                x[e].s.k_scale.store(ks, r);
+                x[e].s.v_scale.store(vs, r);
+                weights[r] = x[e].s.weight;
+            }
         }
+        __syncthreads();
+    }
+}
+
+template <int DQK, int DV>
+static int cache_evict_d(const CacheEvictArgs& a)
+{
+    const int most = a.table_width << a.c.page_shift;
+    const EvictPlan plan{a.c.Hkv, a.c.page_shift, most, a.table_width, a.c.pages, a.recent, evict_ints(most)};
+    auto run = [&](auto kern) {
+        return launch_kernel(kern, dim3((unsigned)(a.B * a.c.Hkv)), dim3(kThreads), 0, a.stream, (uint8_t*)a.c.k, (uint8_t*)a.c.k_scale, (uint8_t*)a.c.v,
+                             (uint8_t*)a.c.v_scale, a.weights, a.table, a.lens, a.keep, a.lens_out, plan, a.places) == hipSuccess ? 0 : -3;
     };
-    // movers into holes: nothing that is written is read
-    for (int64_t i = tid; i < (int64_t)moves * pieces; i += kThreads) {
-        const int m = (int)(i / pieces), piece = (int)(i - (int64_t)m * pieces);
-        Piece x;
-        load(x, row_of(places[moves + m]), piece);
-        store(x, row_of(places[m]), piece);
-    }
-    // the recent rows: what a turn writes may be what it and earlier ones have read, never what later ones will
-    for (int64_t i0 = 0; i0 < (int64_t)recent * pieces; i0 += kThreads) {
-        __syncthreads();
-        const int64_t i = i0 + tid;
-        const int m = (int)(i / pieces), piece = (int)(i - (int64_t)m * pieces);
-        Piece x;
-        if (m < recent) load(x, row_of(of + m), piece);
-        __syncthreads();
-        if (m < recent) store(x, row_of(stay + m), piece);
-    }
+    return a.c.bits == 4 ? run(attn_cache_evict_kernel<DQK, DV, 4>) : run(attn_cache_evict_kernel<DQK, DV, 8>);
 }
 
 }  // namespace
 
 int launch_cache_evict(const CacheEvictArgs& a)
 {
-    const int most = a.table_width << a.c.page_shift;
-    const EvictPlan plan{a.c.Hkv, a.c.page_shift, most, a.table_width, a.c.pages, a.recent, a.c.d_qk * a.c.bits / 8, a.c.d_v * a.c.bits / 8, a.c.d_qk / 32,
-                         a.c.d_v / 32, evict_ints(most)};
-    return launch_kernel(attn_cache_evict_kernel, dim3((unsigned)(a.B * a.c.Hkv)), dim3(kThreads), 0, a.stream, (uint8_t*)a.c.k, (uint8_t*)a.c.k_scale,
-                         (uint8_t*)a.c.v, (uint8_t*)a.c.v_scale, a.weights, a.table, a.lens, a.keep, a.lens_out, plan, a.places) == hipSuccess ? 0 : -3;
+    if (a.c.d_qk == 64 && a.c.d_v == 64) return cache_evict_d<64, 64>(a);
+    if (a.c.d_qk == 96 && a.c.d_v == 96) return cache_evict_d<96, 96>(a);
+    if (a.c.d_qk == 128 && a.c.d_v == 128) return cache_evict_d<128, 128>(a);
+    if (a.c.d_qk == 192 && a.c.d_v == 128) return cache_evict_d<192, 128>(a);
+    if (a.c.d_qk == 256 && a.c.d_v == 256) return cache_evict_d<256, 256>(a);
+    return -2;
 }
 
 }  // namespace attn
