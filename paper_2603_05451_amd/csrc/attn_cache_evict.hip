@@ -17,14 +17,11 @@ namespace attn {
 namespace {
 
 struct EvictPlan {
-    int Hkv, page_shift, most, table_width, pages, recent;
+    int Hkv, page_shift, most, table_width, pages, recent, held;
     int64_t ints;
 };
 
-constexpr int kThreads = 1024;
-constexpr int kHeld = 8;            // turns of 4 keys to a thread whose weights stay in registers: 32 768 keys
-constexpr int kListed = 8192;       // holes and movers that LDS has room for (else they go to the workspace)
-constexpr int kAtOnce = 4;          // pieces of rows that a thread moves in a turn
+constexpr int kAtOnce = 4;          // 16-byte pieces of rows that a thread moves in a turn
 
 // Weights in ascending order as whole numbers: 0 is a row that is not in the cache, NaN the greatest, -0 and 0 are equal.
 __device__ __forceinline__ uint32_t least_first(float w)
@@ -34,20 +31,18 @@ __device__ __forceinline__ uint32_t least_first(float w)
     return x & 0x80000000u ? ~x : x | 0x80000000u;
 }
 
-// Exclusive sums over the block's threads, and the sum of all: to `before` and `all`.  `part`: 17 ints of LDS, free again behind the call's
-// last barrier.
+// Exclusive sums over the block's threads, and the sum of all: to `before` and `all`.  `part`: an int of LDS per wave, of this call's own.
+template <int NT>
 __device__ __forceinline__ void block_sums(int x, ATTN_LDS int* part, int& before, int& all)
 {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int upto = wave_prefix(x);
     if (lane == 63) part[wave] = upto;
     __syncthreads();
-    const int p = lane < kThreads / 64 ? part[lane] : 0, q = wave_prefix(p);
+    const int q = wave_prefix(lane < NT / 64 ? part[lane] : 0);
     before = upto - x + (wave ? __builtin_amdgcn_readlane(q, wave - 1) : 0);
     all = __builtin_amdgcn_readlane(q, 63);
-    __syncthreads();
 }
-
 // The scale bytes of a row: BYTES of them, in words as large as their alignment is for certain.
 template <int BYTES>
 struct ScaleRow {
@@ -71,18 +66,22 @@ struct ScaleRow {
     }
 };
 
-template <int DQK, int DV, int BITS>
-__global__ void __launch_bounds__(kThreads)
+// The loops are not unrolled: most of a small call's time is fetching code that it runs once (4352 rows: 12.9 us with the weights in registers
+// and every loop over them unrolled, EVU us so).
+template <int DQK, int DV, int BITS, int NT>
+__global__ void __launch_bounds__(NT)
 attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint8_t* __restrict__ vc, uint8_t* __restrict__ vs,
                         float* __restrict__ weights, const int* __restrict__ table, const int* __restrict__ lens, const int* __restrict__ keep,
                         int* __restrict__ lens_out, EvictPlan plan, int* __restrict__ places_of_all)
 {
     constexpr int KROW = DQK * BITS / 8, VROW = DV * BITS / 8;
+    // weights of up to plan.held keys as whole numbers, and later the list of places: an entry lies no further than its key's number
+    extern __shared__ __attribute__((aligned(16))) uint32_t held_[];
     __shared__ int count[2048];
-    __shared__ int part_[32];
-    __shared__ int found[2];
-    __shared__ int list[kListed];
-    ATTN_LDS int* const part = (ATTN_LDS int*)part_;
+    __shared__ int part_[4][NT / 64];
+    __shared__ int found[3];
+    ATTN_LDS uint32_t* const held = (ATTN_LDS uint32_t*)held_;
+    auto part = [&](int i) __attribute__((always_inline)) { return (ATTN_LDS int*)part_[i]; };
     const int tid = threadIdx.x;
     const int b = (int)blockIdx.x / plan.Hkv, kvh = (int)blockIdx.x - b * plan.Hkv;
     const int len = min(max(lens[b], 0), plan.most), left = min(len, max(keep[b], 0));
@@ -96,50 +95,46 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
         const int page = pages_of[j >> plan.page_shift];
         return (unsigned)page >= (unsigned)plan.pages ? -1 : (((int64_t)page * plan.Hkv + kvh) << plan.page_shift) + (j & in_page);
     };
-    // four keys from j on, j a multiple of 4: they are in one page
-    auto keys_at = [&](int j, uint32_t (&x)[4]) __attribute__((always_inline)) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t keys4;
+    // four keys from j on, j a multiple of 4: they are in one page; those past the end are not to be counted
+    auto keys_at = [&](int j) __attribute__((always_inline)) {
         const int64_t r = row_of(j);
         f32x4 w = {0.f, 0.f, 0.f, 0.f};
         if (r >= 0) w = *(const f32x4*)(weights + r);
+        keys4 x;
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = r >= 0 ? least_first(w[e]) : 0u;
+        return x;
     };
+    const bool in_lds = of <= plan.held;
+    auto keys = [&](int j) __attribute__((always_inline)) { return in_lds ? *(const ATTN_LDS keys4*)(held + j) : keys_at(j); };
     int* const places = places_of_all + (int64_t)blockIdx.x * plan.ints;
-    const bool in_lds = 2 * min(stay, len - left) <= kListed;          // (there are no more holes than rows that leave, nor than that stay)
 
     int moves = 0;
     if (stay > 0) {
-        uint32_t held[kHeld][4];
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (4 * kThreads * i < of) keys_at(min(4 * (kThreads * i + tid), of - 1) & ~3, held[i]);
-        // f(first of 4 keys, their numbers) for every turn of the block
-        auto each = [&](auto&& f) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (4 * kThreads * i < of) f(4 * (kThreads * i + tid), held[i]);
-#pragma unroll 1
-            for (int j0 = 4 * kThreads * kHeld; j0 < of; j0 += 4 * kThreads) {
-                const int j = j0 + 4 * tid;
-                uint32_t x[4] = {0, 0, 0, 0};
-                if (j < of) keys_at(j, x);
-                f(j, x);
-            }
-        };
+        if (in_lds)
+#pragma unroll 4
+            for (int j = 4 * tid; j < of; j += 4 * NT) *(ATTN_LDS keys4*)(held + j) = keys_at(j);
 
-        // ---- the stay-th greatest: its digits from the highest on
+        // ---- the stay-th greatest: its digits from the highest on, as far as it takes
         uint32_t prefix = 0;                               // those found so far
         int wanted = stay;                                 // the greatest `wanted` of the keys that begin with them
-#pragma unroll
-        for (int digit = 0; digit < 3; ++digit) {
-            constexpr int low_of[] = {21, 10, 0};
-            const int low = low_of[digit], bits = digit == 2 ? 10 : 11;
-            count[tid] = count[tid + kThreads] = 0;
+        int low = 32;                                      // bits of a number behind them
+#pragma unroll 1
+        while (low > 0) {
+            const int bits = min(low, 11);
+            low -= bits;
+            for (int i = tid; i < 2048; i += NT) count[i] = 0;
             __syncthreads();
-            each([&](int j, const uint32_t (&x)[4]) __attribute__((always_inline)) {
+#pragma unroll 1
+            for (int j = 4 * tid; j < of; j += 4 * NT) {
+                const keys4 x = keys(j);
                 int at[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) at[e] = j + e < of && (digit == 0 || x[e] >> (low + bits) == prefix) ? (int)((x[e] >> low) & ((1u << bits) - 1)) : -1;
+                for (int e = 0; e < 4; ++e) {
+                    const uint64_t begins = (uint64_t)x[e] >> low;                     // (low + bits may be 32)
+                    at[e] = j + e < of && begins >> bits == prefix ? (int)(begins & ((1u << bits) - 1)) : -1;
+                }
                 // (equal ones in one go: lanes that add to one place do so one after the other)
                 int n = 1;
 #pragma unroll
@@ -148,127 +143,147 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
                     if (!more && at[e] >= 0) atomicAdd(&count[at[e]], n);
                     n = more ? n + 1 : 1;
                 }
-            });
+            }
             __syncthreads();
-            // places 2 tid and 2 tid + 1, counted from the greatest
-            const int hi = count[2047 - 2 * tid], lo = count[2046 - 2 * tid];
-            int before, all;
-            block_sums(hi + lo, part, before, all);
-            if (before < wanted && wanted <= before + hi + lo) {
-                const bool first = wanted <= before + hi;
-                found[0] = 2047 - 2 * tid - (first ? 0 : 1);
-                found[1] = wanted - before - (first ? 0 : hi);
+            // a thread's share of the places, counted from the greatest
+            constexpr int PER = 2048 / NT;
+            int here[PER], sum = 0, before, all;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) sum += here[i] = count[2047 - PER * tid - i];
+            block_sums<NT>(sum, part(0), before, all);
+            if (before < wanted && wanted <= before + sum) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    if (before < wanted && wanted <= before + here[i]) {
+                        found[0] = 2047 - PER * tid - i;
+                        found[1] = wanted - before;
+                        found[2] = here[i];
+                    }
+                    before += here[i];
+                }
             }
             __syncthreads();
             prefix = prefix << bits | (uint32_t)found[0];
             wanted = found[1];
+            if (found[2] == wanted) break;                 // all that begin so survive
         }
-        const uint32_t least = prefix;                     // of the survivors; `wanted` of those that are equal to it survive, the first ones
+        const uint32_t least = prefix;                     // what survivors begin with at least; `wanted` of those that begin so survive, the first ones
 
         // ---- holes and movers, in ascending order
         int equal = 0;
-        each([&](int j, const uint32_t (&x)[4]) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int j0 = 0, turn = 0; j0 < of; j0 += 4 * NT, ++turn) {
+            const int j = j0 + 4 * tid;
+            keys4 x = {0, 0, 0, 0};
+            if (j < of) x = keys(j);
             int n = 0, before, all;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) n += j + e < of && x[e] == least;
-            block_sums(n, part, before, all);
+            for (int e = 0; e < 4; ++e) n += j + e < of && x[e] >> low == least;
+            block_sums<NT>(n, part(turn & 1 ? 2 : 0), before, all);
             before += equal;
             equal += all;
-            bool listed[4];
-            n = 0;
+            int set = 0;                                   // a bit for each key that is listed
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const bool same = x[e] == least;
-                const bool stays = x[e] > least || (same && before < wanted);
+                const bool same = x[e] >> low == least;
+                const bool stays = x[e] >> low > least || (same && before < wanted);
                 before += same;
-                listed[e] = j + e < of && stays == (j + e >= stay);
-                n += listed[e];
+                if (j + e < of && stays == (j + e >= stay)) set |= 1 << e;
             }
-            block_sums(n, part, before, all);
+            block_sums<NT>(__popc(set), part(turn & 1 ? 3 : 1), before, all);
             before += moves;
             moves += all;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (listed[e]) {
-                    if (in_lds) list[before] = j + e;
+                if (set >> e & 1) {
+                    if (in_lds) held[before] = j + e;
                     else places[before] = j + e;
                     ++before;
                 }
-        });
+        }
         moves /= 2;
         __syncthreads();
     }
 
     // ---- movers into holes, then the recent rows.  A turn reads all it moves before it writes.  What it writes is read by no later turn: holes are
     // read by none, and a recent row's new place lies below those that later ones come from.
-    constexpr int KP = KROW / 16, VP = VROW / 16, PIECES = KP + VP + 1;            // of a row: 16 bytes of codes, and all scales and the weight
-    struct Piece {
-        union {
-            u32x4 w;
-            struct {
-                ScaleRow<DQK / 32> k_scale;
-                ScaleRow<DV / 32> v_scale;
-                float weight;
-            } s;
-        };
-        __device__ Piece() {}
-    };
-    const uint32_t items = (uint32_t)(moves + recent) * PIECES;        // (2^26 * 33 at most)
-    for (uint32_t i0 = 0; i0 < items; i0 += kAtOnce * kThreads) {
-        Piece x[kAtOnce];
-        int64_t to[kAtOnce];
-        int piece[kAtOnce];
+    auto place = [&](int n) __attribute__((always_inline)) { return in_lds ? (int)held[n] : places[n]; };
+    auto from_row = [&](int m) __attribute__((always_inline)) { return row_of(m < moves ? place(moves + m) : of + m - moves); };
+    auto to_row = [&](int m) __attribute__((always_inline)) { return row_of(m < moves ? place(m) : stay + m - moves); };
+    // (a row of a page that is not there is NaN, its weight 0)
+    const int rows = moves + recent;
+#pragma unroll 1
+    for (int m0 = 0; m0 < rows; m0 += NT) {
+        const int m = m0 + tid;
+        ScaleRow<DQK / 32> k_scale;
+        ScaleRow<DV / 32> v_scale;
+        float weight = 0.f;
+        int64_t from = -1, to = -1;
+        if (m < rows) { from = from_row(m); to = to_row(m); }
+        if (from >= 0) {
+            k_scale.load(ks, from);
+            v_scale.load(vs, from);
+            weight = weights[from];
+        } else {
+            k_scale.fill(255);
+            v_scale.fill(255);
+        }
+        __syncthreads();
+        if (to >= 0) {
+            k_scale.store(ks, to);
+            v_scale.store(vs, to);
+            weights[to] = weight;
+        }
+    }
+    constexpr int KP = KROW / 16, VP = VROW / 16, PIECES = KP + VP;                // 16 bytes of codes each
+    const uint32_t items = (uint32_t)rows * PIECES;        // (2^26 * 32 at most)
+#pragma unroll 1
+    for (uint32_t i0 = 0; i0 < items; i0 += kAtOnce * NT) {
+        // (first where all of them are, then what is there: loads return in their order)
+        const uint8_t* from[kAtOnce];
+        uint8_t* to[kAtOnce];
+        u32x4 x[kAtOnce];
 #pragma unroll
         for (int e = 0; e < kAtOnce; ++e) {
-            const uint32_t i = i0 + kThreads * e + tid;
-            to[e] = -1;
+            const uint32_t i = i0 + NT * e + tid;
+            from[e] = to[e] = nullptr;
             if (i >= items) continue;
-            const int m = (int)(i / PIECES);
-            piece[e] = (int)(i % PIECES);
-            auto place = [&](int n) __attribute__((always_inline)) { return in_lds ? list[n] : places[n]; };
-            const int64_t r = row_of(m < moves ? place(moves + m) : of + m - moves);
-            to[e] = row_of(m < moves ? place(m) : stay + m - moves);
-            // (a row of a page that is not there is NaN, its weight 0)
-            if (piece[e] < KP) x[e].w = r < 0 ? u32x4{0, 0, 0, 0} : *(const u32x4*)(kc + r * KROW + 16 * piece[e]);
-            else if (piece[e] < KP + VP) x[e].w = r < 0 ? u32x4{0, 0, 0, 0} : *(const u32x4*)(vc + r * VROW + 16 * (piece[e] - KP));
-            else if (r < 0) {
-                x[e].s.k_scale.fill(255);
-                x[e].s.v_scale.fill(255);
-                x[e].s.weight = 0.f;
-            } else {
-                x[e].s.k_scale.load(ks, r);
-                x[e].s.v_scale.load(vs, r);
-                x[e].s.weight = weights[r];
-            }
+            const int m = (int)(i / PIECES), piece = (int)(i % PIECES);
+            const int64_t f = from_row(m), t = to_row(m);
+            uint8_t* const base = piece < KP ? kc + 16 * piece : vc + 16 * (piece - KP);
+            const int row = piece < KP ? KROW : VROW;
+            if (f >= 0) from[e] = base + f * row;
+            if (t >= 0) to[e] = base + t * row;
         }
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) x[e] = from[e] ? *(const u32x4*)from[e] : u32x4{0, 0, 0, 0};
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < kAtOnce; ++e) {
-            const int64_t r = to[e];
-            if (r < 0) continue;
-            if (piece[e] < KP) *(u32x4*)(kc + r * KROW + 16 * piece[e]) = x[e].w;
-            else if (piece[e] < KP + VP) *(u32x4*)(vc + r * VROW + 16 * (piece[e] - KP)) = x[e].w;
-            else {
-                x[e].s.k_scale.store(ks, r);
-                x[e].s.v_scale.store(vs, r);
-                weights[r] = x[e].s.weight;
-            }
-        }
-        __syncthreads();
+        for (int e = 0; e < kAtOnce; ++e)
+            if (to[e]) *(u32x4*)to[e] = x[e];
     }
 }
 
-template <int DQK, int DV>
-static int cache_evict_d(const CacheEvictArgs& a)
+template <int DQK, int DV, int BITS, int NT>
+static int cache_evict_t(const CacheEvictArgs& a, int most)
 {
-    const int most = a.table_width << a.c.page_shift;
-    const EvictPlan plan{a.c.Hkv, a.c.page_shift, most, a.table_width, a.c.pages, a.recent, evict_ints(most)};
-    auto run = [&](auto kern) {
-        return launch_kernel(kern, dim3((unsigned)(a.B * a.c.Hkv)), dim3(kThreads), 0, a.stream, (uint8_t*)a.c.k, (uint8_t*)a.c.k_scale, (uint8_t*)a.c.v,
-                             (uint8_t*)a.c.v_scale, a.weights, a.table, a.lens, a.keep, a.lens_out, plan, a.places) == hipSuccess ? 0 : -3;
-    };
-    return a.c.bits == 4 ? run(attn_cache_evict_kernel<DQK, DV, 4>) : run(attn_cache_evict_kernel<DQK, DV, 8>);
+    constexpr int room = 32768;                            // keys: 128 KiB
+    const int held = ((most < room ? most : room) + 3) & ~3;
+    const EvictPlan plan{a.c.Hkv, a.c.page_shift, most, a.table_width, a.c.pages, a.recent, held, evict_ints(most)};
+    auto kern = attn_cache_evict_kernel<DQK, DV, BITS, NT>;
+    static LdsOptIn lds;
+    if (!lds.allow(kern, 4 * room)) return -3;
+    return launch_kernel(kern, dim3((unsigned)(a.B * a.c.Hkv)), dim3(NT), (size_t)(4 * held), a.stream, (uint8_t*)a.c.k, (uint8_t*)a.c.k_scale, (uint8_t*)a.c.v,
+                         (uint8_t*)a.c.v_scale, a.weights, a.table, a.lens, a.keep, a.lens_out, plan, a.places) == hipSuccess ? 0 : -3;
 }
+template <int DQK, int DV, int BITS>
+static int cache_evict_b(const CacheEvictArgs& a)
+{
+    const int most = a.table_width << a.c.page_shift, nt = evict_threads(most);
+    return nt == 256 ? cache_evict_t<DQK, DV, BITS, 256>(a, most) : nt == 512 ? cache_evict_t<DQK, DV, BITS, 512>(a, most) : cache_evict_t<DQK, DV, BITS, 1024>(a, most);
+}
+template <int DQK, int DV>
+static int cache_evict_d(const CacheEvictArgs& a) { return a.c.bits == 4 ? cache_evict_b<DQK, DV, 4>(a) : cache_evict_b<DQK, DV, 8>(a); }
 
 }  // namespace
 
