@@ -21,6 +21,7 @@ struct EvictPlan {
     int64_t ints;
 };
 
+constexpr int NT = 1024;            // (512 are slower from some thousand rows on, 4352 rows 13.7 and 11.3 us, and no faster for few)
 constexpr int kAtOnce = 4;          // 16-byte pieces of rows that a thread moves in a turn
 
 // Weights in ascending order as whole numbers: 0 is a row that is not in the cache, NaN the greatest, -0 and 0 are equal.
@@ -32,7 +33,6 @@ __device__ __forceinline__ uint32_t least_first(float w)
 }
 
 // Exclusive sums over the block's threads, and the sum of all: to `before` and `all`.  `part`: an int of LDS per wave, of this call's own.
-template <int NT>
 __device__ __forceinline__ void block_sums(int x, ATTN_LDS int* part, int& before, int& all)
 {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -67,8 +67,8 @@ struct ScaleRow {
 };
 
 // The loops are not unrolled: most of a small call's time is fetching code that it runs once (4352 rows: 12.9 us with the weights in registers
-// and every loop over them unrolled, EVU us so).
-template <int DQK, int DV, int BITS, int NT>
+// and every loop over them unrolled, 11.1 us so).
+template <int DQK, int DV, int BITS>
 __global__ void __launch_bounds__(NT)
 attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint8_t* __restrict__ vc, uint8_t* __restrict__ vs,
                         float* __restrict__ weights, const int* __restrict__ table, const int* __restrict__ lens, const int* __restrict__ keep,
@@ -118,7 +118,7 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
 
         // ---- the stay-th greatest: its digits from the highest on, as far as it takes
         uint32_t prefix = 0;                               // those found so far
-        int wanted = stay;                                 // the greatest `wanted` of the keys that begin with them
+        int wanted = stay, same = 0;                       // the greatest `wanted` of the keys that begin with them, which are `same`
         int low = 32;                                      // bits of a number behind them
 #pragma unroll 1
         while (low > 0) {
@@ -150,7 +150,7 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
             int here[PER], sum = 0, before, all;
 #pragma unroll
             for (int i = 0; i < PER; ++i) sum += here[i] = count[2047 - PER * tid - i];
-            block_sums<NT>(sum, part(0), before, all);
+            block_sums(sum, part(0), before, all);
             if (before < wanted && wanted <= before + sum) {
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
@@ -165,7 +165,8 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
             __syncthreads();
             prefix = prefix << bits | (uint32_t)found[0];
             wanted = found[1];
-            if (found[2] == wanted) break;                 // all that begin so survive
+            same = found[2];
+            if (same == wanted) break;                     // all that begin so survive
         }
         const uint32_t least = prefix;                     // what survivors begin with at least; `wanted` of those that begin so survive, the first ones
 
@@ -176,21 +177,24 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
             const int j = j0 + 4 * tid;
             keys4 x = {0, 0, 0, 0};
             if (j < of) x = keys(j);
-            int n = 0, before, all;
+            int before = 0, all;
+            if (same != wanted) {                          // ties: the first ones survive
+                int n = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) n += j + e < of && x[e] >> low == least;
-            block_sums<NT>(n, part(turn & 1 ? 2 : 0), before, all);
-            before += equal;
-            equal += all;
+                for (int e = 0; e < 4; ++e) n += j + e < of && x[e] >> low == least;
+                block_sums(n, part(turn & 1 ? 2 : 0), before, all);
+                before += equal;
+                equal += all;
+            }
             int set = 0;                                   // a bit for each key that is listed
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const bool same = x[e] >> low == least;
-                const bool stays = x[e] >> low > least || (same && before < wanted);
-                before += same;
+                const bool is = x[e] >> low == least;
+                const bool stays = x[e] >> low > least || (is && (same == wanted || before < wanted));
+                before += is;
                 if (j + e < of && stays == (j + e >= stay)) set |= 1 << e;
             }
-            block_sums<NT>(__popc(set), part(turn & 1 ? 3 : 1), before, all);
+            block_sums(__popc(set), part(turn & 1 ? 3 : 1), before, all);
             before += moves;
             moves += all;
 #pragma unroll
@@ -264,23 +268,17 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
     }
 }
 
-template <int DQK, int DV, int BITS, int NT>
-static int cache_evict_t(const CacheEvictArgs& a, int most)
+template <int DQK, int DV, int BITS>
+static int cache_evict_b(const CacheEvictArgs& a)
 {
     constexpr int room = 32768;                            // keys: 128 KiB
-    const int held = ((most < room ? most : room) + 3) & ~3;
+    const int most = a.table_width << a.c.page_shift, held = ((most < room ? most : room) + 3) & ~3;
     const EvictPlan plan{a.c.Hkv, a.c.page_shift, most, a.table_width, a.c.pages, a.recent, held, evict_ints(most)};
-    auto kern = attn_cache_evict_kernel<DQK, DV, BITS, NT>;
+    auto kern = attn_cache_evict_kernel<DQK, DV, BITS>;
     static LdsOptIn lds;
     if (!lds.allow(kern, 4 * room)) return -3;
     return launch_kernel(kern, dim3((unsigned)(a.B * a.c.Hkv)), dim3(NT), (size_t)(4 * held), a.stream, (uint8_t*)a.c.k, (uint8_t*)a.c.k_scale, (uint8_t*)a.c.v,
                          (uint8_t*)a.c.v_scale, a.weights, a.table, a.lens, a.keep, a.lens_out, plan, a.places) == hipSuccess ? 0 : -3;
-}
-template <int DQK, int DV, int BITS>
-static int cache_evict_b(const CacheEvictArgs& a)
-{
-    const int most = a.table_width << a.c.page_shift, nt = evict_threads(most);
-    return nt == 256 ? cache_evict_t<DQK, DV, BITS, 256>(a, most) : nt == 512 ? cache_evict_t<DQK, DV, BITS, 512>(a, most) : cache_evict_t<DQK, DV, BITS, 1024>(a, most);
 }
 template <int DQK, int DV>
 static int cache_evict_d(const CacheEvictArgs& a) { return a.c.bits == 4 ? cache_evict_b<DQK, DV, 4>(a) : cache_evict_b<DQK, DV, 8>(a); }

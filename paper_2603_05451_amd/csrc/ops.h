@@ -2,7 +2,6 @@
 // share their work out (arithmetic on sizes alone, without HIP for a host compiler).
 #pragma once
 #include <stdint.h>
-#include <stdlib.h>
 
 namespace attn {
 
@@ -167,7 +166,6 @@ inline int weigh_blocks(int64_t units) { return (int)(units < 4096 ? units : 409
 
 // ---- eviction
 
-inline int evict_threads(int64_t most) { const char* e = getenv("EVT"); if (e) return atoi(e); return most <= 8192 ? 256 : 1024; }
 inline int64_t evict_ints(int64_t most) { return (most + 3) / 4 * 4; }     // of a (sequence, KV head)'s list of places
 
 }  // namespace attn
