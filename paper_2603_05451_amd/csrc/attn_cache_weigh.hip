@@ -22,20 +22,34 @@ struct WeighSeq {
 struct WeighPlace {
     WeighSeq s;
     int b, group;               // sequence, and which group of its keys
+    int group_keys;
 };
 
-// Group `u` of all sequences' keys, of `keys` each; false behind the last one.
+__device__ __forceinline__ WeighSeq weigh_seq(const WeighPlan& p, const int* __restrict__ cu, const int* __restrict__ lens, int b)
+{
+    if (b >= p.B) return {0, 0, 0};
+    const int q0 = cu ? cu[b] : b * p.Nq, q1 = cu ? cu[b + 1] : q0 + p.Nq;
+    if (q0 < 0 || q1 <= q0 || q1 > p.T) return {0, 0, 0};
+    return {q0, q1 - q0, min(max(lens[b], 0), p.most)};
+}
+// Steps of KEYS keys in a group: one of many rows; of few rows as many as make about a round of groups of all such sequences.
 template <int KEYS>
-__device__ __forceinline__ bool weigh_find(const WeighPlan& p, const int* __restrict__ cu, const int* __restrict__ lens, int u, WeighPlace& at)
+__device__ __forceinline__ int weigh_few_steps(const WeighPlan& p, const int* __restrict__ cu, const int* __restrict__ lens)
+{
+    float total = 0.f;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const WeighSeq s = weigh_seq(p, cu, lens, b0 + (threadIdx.x & 63));
+        total += s.nq * p.G <= kWeighFew ? (float)((s.len + KEYS - 1) / KEYS) : 0.f;
+    }
+    return max(1, (int)ceilf(wave_sum(total) * (float)p.Hkv * (1.0f / kWeighRound)));
+}
+// Group `u` of all sequences' keys; false behind the last one.
+template <int KEYS>
+__device__ __forceinline__ bool weigh_find(const WeighPlan& p, const int* __restrict__ cu, const int* __restrict__ lens, int few_steps, int u, WeighPlace& at)
 {
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int b = b0 + (threadIdx.x & 63);
-        WeighSeq s{0, 0, 0};
-        if (b < p.B) {
-            const int q0 = cu ? cu[b] : b * p.Nq, q1 = cu ? cu[b + 1] : q0 + p.Nq;
-            if (q0 >= 0 && q1 > q0 && q1 <= p.T) s = {q0, q1 - q0, min(max(lens[b], 0), p.most)};
-        }
-        const int mine = (s.len + KEYS - 1) / KEYS, upto = wave_prefix(mine);
+        const WeighSeq s = weigh_seq(p, cu, lens, b0 + (threadIdx.x & 63));
+        const int n = s.nq * p.G <= kWeighFew ? few_steps : 1, steps = (s.len + KEYS - 1) / KEYS, mine = (steps + n - 1) / n, upto = wave_prefix(mine);
         const uint64_t past = __ballot(upto > u);
         if (past) {
             const int l = __builtin_ctzll(past);
@@ -43,6 +57,7 @@ __device__ __forceinline__ bool weigh_find(const WeighPlan& p, const int* __rest
             at.s = {of(s.q0), of(s.nq), of(s.len)};
             at.b = b0 + l;
             at.group = u - (of(upto) - of(mine));
+            at.group_keys = KEYS * of((steps + max(mine, 1) - 1) / max(mine, 1));
             return true;
         }
         u -= __builtin_amdgcn_readlane(upto, 63);

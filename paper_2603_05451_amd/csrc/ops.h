@@ -159,10 +159,13 @@ inline ChunkShape chunk_shape(int B, int T, int H, int Hkv, int d_qk, int64_t mo
 
 // ---- weights of cached keys
 
-constexpr int weigh_key_blocks(int d_qk) { return d_qk <= 128 ? 2 : 1; }        // of 32 keys to a wave
-constexpr int weigh_keys(int d_qk) { return 4 * 32 * weigh_key_blocks(d_qk); }  // of a block
+constexpr int kWeighFew = 32;           // a sequence with no more rows goes by the body for few
+constexpr int weigh_key_blocks(int d_qk) { return d_qk <= 128 ? 2 : 1; }        // of 32 keys that a wave takes together
+constexpr int weigh_keys(int d_qk) { return 4 * 32 * weigh_key_blocks(d_qk); }  // of a block (of few rows: in one step)
+constexpr int weigh_rows(int d_qk) { return d_qk <= 128 ? 64 : 32; }            // of a tile of queries: 32 KiB of LDS at d = 128, twice
+constexpr int kWeighRound = 2 * 256;    // blocks that the chip holds
 inline int64_t weigh_units(int B, int Hkv, int d_qk, int64_t most) { return (int64_t)B * Hkv * ((most + weigh_keys(d_qk) - 1) / weigh_keys(d_qk)); }
-inline int weigh_blocks(int64_t units) { return (int)(units < 4096 ? units : 4096); }
+inline int weigh_blocks(int64_t units) { return (int)(units < 2 * kWeighRound ? units : 2 * kWeighRound); }
 
 // ---- eviction
 
