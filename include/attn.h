@@ -373,10 +373,13 @@ int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, co
  *   - A query with lse = -inf (it saw no key) adds nothing.  A key that is not finite has the weight NaN.  Entries of the table that are
  *     outside the cache are passed over.  Weights of other rows are not touched.
  *   - Every row of the cache may belong to one sequence at most (a page that two sequences share has unspecified weights).
- *   - Sums are in fp32, in an order that depends on the sizes and lengths alone.  One kernel, no workspace.  Limits as in the two calls. */
+ *   - Sums are in fp32, in an order that depends on the sizes and lengths alone.  Limits as in the two calls.
+ *   workspace: attn_cache_weigh_workspace_bytes(...) bytes (packed: whether there are cu_seqlens), 256-byte aligned, contents ignored.  One kernel, and
+ *   one that adds up where there are rows enough for them to be divided over blocks (without which the weights of such sequences are untouched). */
+size_t attn_cache_weigh_workspace_bytes(const attn_cache_t* cache, int B, int Nq, int H, int table_width, int packed);
 int attn_cache_weigh(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, const float* lse, float* weights,
                      const int* block_table, int table_width, const int* cu_seqlens, const int* lens, int B, int Nq, int H, float scale, int causal,
-                     int fresh, void* stream);
+                     int fresh, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Eviction by those weights: of every sequence with more than keep[b] rows (int32, device; a negative number counts as 0) that many stay, for each KV
  * head by itself: the last `recent` (no more than keep[b]), and of the others those with the greatest weights (ties: the first; NaN is the greatest,

@@ -103,7 +103,9 @@ def lib():
         L.attn_cache_chunk_workspace_bytes.restype = sz
         L.attn_cache_chunk_fwd.argtypes = [i, cp, vp, sp, vp, sp, vp, vp, i, vp, vp, i, i, i, f, i, vp, sz, vp]
         L.attn_cache_chunk_fwd.restype = i
-        L.attn_cache_weigh.argtypes = [i, cp, vp, sp, vp, vp, vp, i, vp, vp, i, i, i, f, i, i, vp]
+        L.attn_cache_weigh_workspace_bytes.argtypes = [cp, i, i, i, i, i]
+        L.attn_cache_weigh_workspace_bytes.restype = sz
+        L.attn_cache_weigh.argtypes = [i, cp, vp, sp, vp, vp, vp, i, vp, vp, i, i, i, f, i, i, vp, sz, vp]
         L.attn_cache_weigh.restype = i
         L.attn_cache_evict_workspace_bytes.argtypes = [cp, i, i]
         L.attn_cache_evict_workspace_bytes.restype = sz
@@ -124,8 +126,8 @@ def lib():
                                              L.attn_varlen_bwd_dtype, L.attn_varlen_workspace_bytes, L.attn_fwd_strided, L.attn_bwd_strided,
                                              L.attn_strided_workspace_bytes, L.attn_rope_fwd, L.attn_rope_bwd, L.attn_rope_workspace_bytes,
                                              L.attn_cache_write, L.attn_cache_read, L.attn_cache_fwd, L.attn_cache_workspace_bytes,
-                                             L.attn_cache_chunk_fwd, L.attn_cache_chunk_workspace_bytes, L.attn_cache_weigh, L.attn_cache_evict,
-                                             L.attn_cache_evict_workspace_bytes)),
+                                             L.attn_cache_chunk_fwd, L.attn_cache_chunk_workspace_bytes, L.attn_cache_weigh,
+                                             L.attn_cache_weigh_workspace_bytes, L.attn_cache_evict, L.attn_cache_evict_workspace_bytes)),
                       torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.nn.Parameter)
         _native = _binding
         _lib = L                # last: another thread that finds it set uses both
@@ -810,12 +812,16 @@ def _weights(weights, layout, stream):
     return _dev(weights, "weights", (layout.pages, layout.Hkv, layout.page), torch.float32)
 
 
-def attn_cache_weigh(q, lse, weights, cache, block_table, lens, scale, causal, cu_seqlens=None, fresh=False, stream=None):
+def attn_cache_weigh_workspace_bytes(cache, B, Nq, H, table_width, packed) -> int:
+    return int(lib().attn_cache_weigh_workspace_bytes(ctypes.byref(_cache(cache, None)), B, Nq, H, table_width, int(bool(packed))))
+
+
+def attn_cache_weigh(q, lse, weights, cache, block_table, lens, scale, causal, cu_seqlens=None, fresh=False, workspace=None, stream=None):
     """Adds to weights (fp32 [pages,Hkv,page], attn_cache_weights) the attention weight that each key of the sequences had from the queries of an
     attn_cache_chunk_fwd call (q [T,H,d_qk], its lse [H,T], its cu_seqlens) or an attn_cache_fwd call (q [B,Nq,H,d_qk], its lse [B,H,Nq], no
     cu_seqlens), summed over queries and the heads of a KV head's group; the other arguments are that call's.  fresh: the last keys, as many as the
     sequence has queries, are the call's own, their weights are set and not added to.  -> weights"""
-    r = (_native or _call()).cache_weigh(q, lse, weights, cache, block_table, lens, scale, causal, cu_seqlens, fresh, stream)
+    r = (_native or _call()).cache_weigh(q, lse, weights, cache, block_table, lens, scale, causal, cu_seqlens, fresh, workspace, stream)
     if r is not None:
         _check(r)
         return weights
@@ -833,8 +839,13 @@ def attn_cache_weigh(q, lse, weights, cache, block_table, lens, scale, causal, c
     cu = None if cu_seqlens is None else _indexes(cu_seqlens, "cu_seqlens", (B + 1,), stream)
     _here(lse, "lse", torch.float32, stream)
     lse_p = _dev_lse(lse, (B, H, N), "B,H,Nq") if cu is None else _dev_lse(lse, (H, N), "H,T")
+    if workspace is None:
+        need = lib().attn_cache_weigh_workspace_bytes(ctypes.byref(layout), B, N, H, width, int(cu is not None))
+        workspace = _empty((max(need, 256),), torch.uint8, q.device, stream)
+    else:
+        _scratch(workspace, stream)
     _check(lib().attn_cache_weigh(code, ctypes.byref(layout), x.data_ptr(), _strides(x), lse_p, _weights(weights, layout, stream), table, width, cu, keys,
-                                  B, N, H, float(scale), int(bool(causal)), int(bool(fresh)), _stream(stream)))
+                                  B, N, H, float(scale), int(bool(causal)), int(bool(fresh)), workspace.data_ptr(), workspace.numel(), _stream(stream)))
     return weights
 
 

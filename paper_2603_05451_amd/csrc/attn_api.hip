@@ -868,28 +868,47 @@ int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, co
     return rc == 0 ? ATTN_OK : (rc == -2 ? ATTN_EUNSUPPORTED : ATTN_ELAUNCH);
 }
 
+namespace {
+
+int check_cache_weigh(const attn_cache_t* c, int B, int Nq, int H, int table_width, int packed)
+{
+    if (int rc = check_cache_table(c, B, H, table_width)) return rc;
+    if (Nq <= 0) return ATTN_EINVAL;
+    const int64_t T = packed ? Nq : (int64_t)B * Nq;
+    if (T * H > 1 << 28 || T * H * c->d_qk > 1LL << 34) return ATTN_EUNSUPPORTED;
+    return attn::weigh_shape(B, T, H, c->Hkv, c->d_qk, (int64_t)table_width * c->page).units > 1 << 28 ? ATTN_EUNSUPPORTED : ATTN_OK;
+}
+
+}  // namespace
+
+size_t attn_cache_weigh_workspace_bytes(const attn_cache_t* cache, int B, int Nq, int H, int table_width, int packed)
+{
+    if (check_cache_weigh(cache, B, Nq, H, table_width, packed) != ATTN_OK) return 0;
+    const attn::WeighShape s = attn::weigh_shape(B, packed ? Nq : (int64_t)B * Nq, H, cache->Hkv, cache->d_qk, (int64_t)table_width * cache->page);
+    return s.split ? align_up((size_t)s.units * (size_t)attn::weigh_keys(cache->d_qk) * sizeof(float), 256) : 256;
+}
+
 int attn_cache_weigh(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, const float* lse, float* weights,
                      const int* block_table, int table_width, const int* cu_seqlens, const int* lens, int B, int Nq, int H, float scale, int causal,
-                     int fresh, void* stream)
+                     int fresh, void* workspace, size_t workspace_bytes, void* stream)
 {
     if (dtype != ATTN_BF16 && dtype != ATTN_F16) return ATTN_EUNSUPPORTED;
-    if (!q || !lse || !weights || !block_table || !lens) return ATTN_EINVAL;
-    if (int rc = check_cache_table(cache, B, H, table_width)) return rc;
-    if (Nq <= 0) return ATTN_EINVAL;
-    const int64_t T = cu_seqlens ? Nq : (int64_t)B * Nq;
-    if (T * H > 1 << 28 || T * H * cache->d_qk > 1LL << 34) return ATTN_EUNSUPPORTED;
-    if (attn::weigh_units(B, cache->Hkv, cache->d_qk, (int64_t)table_width * cache->page) > 1 << 30) return ATTN_EUNSUPPORTED;
-    if (bad_view(sq, cu_seqlens ? 1 : B, Nq, H)) return ATTN_EINVAL;
+    if (!q || !lse || !weights || !block_table || !lens || !workspace) return ATTN_EINVAL;
+    const int packed = cu_seqlens != nullptr;
+    if (int rc = check_cache_weigh(cache, B, Nq, H, table_width, packed)) return rc;
+    if (bad_view(sq, packed ? 1 : B, Nq, H)) return ATTN_EINVAL;
     if (!(scale > 0.0f) || !(scale < 1e30f)) return ATTN_EINVAL;
-    if (misaligned(q, 16) || misaligned(lse, 4) || misaligned(weights, 16) || misaligned(block_table, 4) || misaligned(cu_seqlens, 4) || misaligned(lens, 4))
+    if (misaligned(q, 16) || misaligned(lse, 4) || misaligned(weights, 16) || misaligned(block_table, 4) || misaligned(cu_seqlens, 4) || misaligned(lens, 4) ||
+        misaligned(workspace, 256))
         return ATTN_EINVAL;
+    if (workspace_bytes < attn_cache_weigh_workspace_bytes(cache, B, Nq, H, table_width, packed)) return ATTN_EINVAL;
     attn::CacheWeighArgs a = {};
     a.c = cache_args(cache);
     a.q = q;
     a.lse = lse;
     a.weights = weights;
     a.sq = as_is(sq);
-    a.lse_batch = cu_seqlens ? 0 : (long long)H * Nq;
+    a.lse_batch = packed ? 0 : (long long)H * Nq;
     a.lse_head = Nq;
     a.table = block_table;
     a.lens = lens;
@@ -897,11 +916,12 @@ int attn_cache_weigh(int dtype, const attn_cache_t* cache, const void* q, const 
     a.table_width = table_width;
     a.B = B;
     a.Nq = Nq;
-    a.T = (int)T;
+    a.T = packed ? Nq : B * Nq;
     a.H = H;
     a.scale = scale;
     a.causal = causal != 0;
     a.fresh = fresh != 0;
+    a.parts = static_cast<float*>(workspace);
     a.f16 = dtype == ATTN_F16;
     a.stream = stream;
     const int rc = attn::launch_cache_weigh(a);

@@ -11,7 +11,7 @@ namespace attn {
 struct WeighPlan {
     int B, Nq, T, G, Hkv, page_shift, most, table_width, pages;
     uint32_t per_g;             // 2^32 / G, rounded up, to divide by G
-    int causal, fresh;
+    int causal, fresh, split;   // split: weigh_shape's
     float scale_log2e;
     Stride3 sq;
     long long lse_batch, lse_head;
@@ -21,8 +21,9 @@ struct WeighSeq {
 };
 struct WeighPlace {
     WeighSeq s;
-    int b, group;               // sequence, and which group of its keys
+    int b, group, groups;       // sequence, and which group of its keys
     int group_keys;
+    int share, shares, share_tiles;     // which share of its tiles of rows
 };
 
 __device__ __forceinline__ WeighSeq weigh_seq(const WeighPlan& p, const int* __restrict__ cu, const int* __restrict__ lens, int b)
@@ -32,38 +33,68 @@ __device__ __forceinline__ WeighSeq weigh_seq(const WeighPlan& p, const int* __r
     if (q0 < 0 || q1 <= q0 || q1 > p.T) return {0, 0, 0};
     return {q0, q1 - q0, min(max(lens[b], 0), p.most)};
 }
-// Steps of KEYS keys in a group: one of many rows; of few rows as many as make about a round of groups of all such sequences.
-template <int KEYS>
-__device__ __forceinline__ int weigh_few_steps(const WeighPlan& p, const int* __restrict__ cu, const int* __restrict__ lens)
-{
-    float total = 0.f;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const WeighSeq s = weigh_seq(p, cu, lens, b0 + (threadIdx.x & 63));
-        total += s.nq * p.G <= kWeighFew ? (float)((s.len + KEYS - 1) / KEYS) : 0.f;
-    }
-    return max(1, (int)ceilf(wave_sum(total) * (float)p.Hkv * (1.0f / kWeighRound)));
-}
-// Group `u` of all sequences' keys; false behind the last one.
-template <int KEYS>
-__device__ __forceinline__ bool weigh_find(const WeighPlan& p, const int* __restrict__ cu, const int* __restrict__ lens, int few_steps, int u, WeighPlace& at)
-{
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const WeighSeq s = weigh_seq(p, cu, lens, b0 + (threadIdx.x & 63));
-        const int n = s.nq * p.G <= kWeighFew ? few_steps : 1, steps = (s.len + KEYS - 1) / KEYS, mine = (steps + n - 1) / n, upto = wave_prefix(mine);
-        const uint64_t past = __ballot(upto > u);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-            at.s = {of(s.q0), of(s.nq), of(s.len)};
-            at.b = b0 + l;
-            at.group = u - (of(upto) - of(mine));
-            at.group_keys = KEYS * of((steps + max(mine, 1) - 1) / max(mine, 1));
-            return true;
+
+// How the sequences' work is shared out, from boundaries and lengths, the same in every wave of a launch (and of the one that adds up).
+template <int KEYS, int RT>
+struct WeighWork {
+    const WeighPlan& p;
+    const int* __restrict__ cu;
+    const int* __restrict__ lens;
+    int few_steps, share_tiles;         // few rows: KEYS keys of a group; many: tiles of rows of a share
+    WeighSeq held;                      // the lane's of the first 64 sequences
+
+    __device__ __forceinline__ WeighSeq seq(int b0) const { return b0 == 0 ? held : weigh_seq(p, cu, lens, b0 + (threadIdx.x & 63)); }
+
+    __device__ __forceinline__ bool few(const WeighSeq& s) const { return s.nq * p.G <= kWeighFew; }
+    __device__ __forceinline__ int steps(const WeighSeq& s) const { return (s.len + KEYS - 1) / KEYS; }
+    __device__ __forceinline__ int tiles(const WeighSeq& s) const { return (s.nq * p.G + RT - 1) / RT; }
+    // Of few rows as many keys to a group as make a round of groups, of many rows as many tiles to a share.
+    __device__ __forceinline__ WeighWork(const WeighPlan& plan, const int* __restrict__ c, const int* __restrict__ l) : p(plan), cu(c), lens(l)
+    {
+        held = weigh_seq(p, cu, lens, threadIdx.x & 63);
+        float of_few = 0.f, of_many = 0.f;
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            const WeighSeq s = seq(b0);
+            const float n = (float)steps(s);
+            if (few(s)) of_few += n;
+            else of_many += n * (float)tiles(s) * (p.causal && s.len > 0 ? 1.f - 0.5f * fminf(1.f, (float)s.nq / (float)s.len) : 1.f);
         }
-        u -= __builtin_amdgcn_readlane(upto, 63);
+        const float of_round = (float)p.Hkv * (1.0f / kWeighRound);
+        few_steps = max(1, (int)ceilf(wave_sum(of_few) * of_round));
+        share_tiles = p.split ? max(4, (int)ceilf(fminf(wave_sum(of_many) * of_round, 1e9f))) : 1 << 30;
     }
-    return false;
-}
+    __device__ __forceinline__ int groups(const WeighSeq& s) const { const int n = few(s) ? few_steps : 1; return (steps(s) + n - 1) / n; }
+    __device__ __forceinline__ int shares(const WeighSeq& s) const { return few(s) ? 1 : max(1, (int)(((int64_t)tiles(s) + share_tiles / 2) / share_tiles)); }
+    // Group (ALL: and share) number u of all sequences'; false behind the last one.  Unit: the first of its sequence's units.
+    template <bool ALL>
+    __device__ __forceinline__ bool find(int u, WeighPlace& at, int& unit) const
+    {
+        unit = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 64) {
+            const WeighSeq s = seq(b0);
+            const int g = groups(s), n = shares(s), mine = ALL ? g * n : g, upto = wave_prefix(mine), units = ALL ? upto : wave_prefix(g * n);
+            const uint64_t past = __ballot(upto > u);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+                at.s = {of(s.q0), of(s.nq), of(s.len)};
+                at.b = b0 + l;
+                at.groups = of(g);
+                at.shares = of(n);
+                const int local = u - (of(upto) - of(mine));
+                at.share = ALL ? local / at.groups : 0;
+                at.group = ALL ? local - at.share * at.groups : local;
+                at.group_keys = KEYS * ((of(steps(s)) + at.groups - 1) / at.groups);
+                at.share_tiles = (of(tiles(s)) + at.shares - 1) / at.shares;
+                unit += of(units) - of(g * n);
+                return true;
+            }
+            u -= __builtin_amdgcn_readlane(upto, 63);
+            unit += __builtin_amdgcn_readlane(units, 63);
+        }
+        return false;
+    }
+};
 
 __device__ __forceinline__ int divide(uint32_t x, uint32_t per_g, int G)       // x / G, for any x
 {

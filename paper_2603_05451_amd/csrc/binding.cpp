@@ -35,6 +35,7 @@ decltype(&attn_cache_workspace_bytes) p_cache_bytes = nullptr;
 decltype(&attn_cache_chunk_fwd) p_cache_chunk = nullptr;
 decltype(&attn_cache_chunk_workspace_bytes) p_chunk_bytes = nullptr;
 decltype(&attn_cache_weigh) p_cache_weigh = nullptr;
+decltype(&attn_cache_weigh_workspace_bytes) p_weigh_bytes = nullptr;
 decltype(&attn_cache_evict) p_cache_evict = nullptr;
 decltype(&attn_cache_evict_workspace_bytes) p_evict_bytes = nullptr;
 PyObject *get_device = nullptr, *get_stream = nullptr;      // torch._C._cuda_getDevice, _cuda_getCurrentRawStream
@@ -735,12 +736,12 @@ PyObject* cache_chunk_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// q, lse, weights, cache, block_table, lens, scale, causal, cu_seqlens, fresh, stream
+// q, lse, weights, cache, block_table, lens, scale, causal, cu_seqlens, fresh, workspace, stream
 PyObject* cache_weigh(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     CallHere c;
-    if (n != 11) NOT_HERE;
+    if (n != 12) NOT_HERE;
     const at::Tensor *q = c.tensor(a[0]), *lse = c.tensor(a[1]), *weights = c.tensor(a[2]), *table = c.tensor(a[4]), *lens = c.tensor(a[5]);
     const at::Tensor* cu = a[8] == Py_None ? nullptr : c.tensor(a[8]);
     c.element(q);
@@ -754,13 +755,18 @@ PyObject* cache_weigh(PyObject*, PyObject* const* a, Py_ssize_t n)
     void *qp = c.rows(q, c.type, at::IntArrayRef(qs + packed, 4 - packed)), *tp = c.flat(table, at::kInt, ts), *np = c.flat(lens, at::kInt, at::IntArrayRef(ts, 1));
     void *lp = c.flat(lse, at::kFloat, at::IntArrayRef(ls + packed, 3 - packed)), *wp = c.flat(weights, at::kFloat, wsh);
     void* up = packed ? c.flat(cu, at::kInt, at::IntArrayRef(&edges, 1)) : nullptr;
-    void* s = c.stream_here(a[10]);
+    at::Tensor ws;
+    if (a[10] != Py_None) { const at::Tensor* t = c.tensor(a[10]); if (t) { ws = *t; if (t->scalar_type() != at::kByte || !t->is_contiguous()) c.ok = false; } }
+    if (!c.ok) NOT_HERE;
+    const size_t need = ws.defined() ? 0 : p_weigh_bytes(&cache, B, N, H, width, packed);
+    void* s = c.stream_here(a[11]);
     if (!c.ok) NOT_HERE;
     int rc;
     {
         Unlocked threads;
+        if (!ws.defined()) ws = make_bytes(*q, need);
         rc = p_cache_weigh(c.dtype, &cache, qp, c.strides, (const float*)lp, (float*)wp, (const int*)tp, width, (const int*)up, (const int*)np, B, N, H,
-                           (float)scale, causal, fresh, s);
+                           (float)scale, causal, fresh, ws.data_ptr(), (size_t)ws.numel(), s);
     }
     return PyLong_FromLong(rc);
     END_HANDLE_TH_ERRORS
@@ -805,7 +811,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
     void** const to[] = {(void**)&p_fwd, (void**)&p_bwd_phases, (void**)&p_bwd_dtype, (void**)&p_bwd_bytes, (void**)&p_varlen_fwd, (void**)&p_varlen_bwd,
                          (void**)&p_varlen_bytes, (void**)&p_fwd_strided, (void**)&p_bwd_strided, (void**)&p_strided_bytes, (void**)&p_rope_fwd, (void**)&p_rope_bwd,
                          (void**)&p_rope_bytes, (void**)&p_cache_write, (void**)&p_cache_read, (void**)&p_cache_fwd, (void**)&p_cache_bytes,
-                         (void**)&p_cache_chunk, (void**)&p_chunk_bytes, (void**)&p_cache_weigh, (void**)&p_cache_evict, (void**)&p_evict_bytes};
+                         (void**)&p_cache_chunk, (void**)&p_chunk_bytes, (void**)&p_cache_weigh, (void**)&p_weigh_bytes, (void**)&p_cache_evict, (void**)&p_evict_bytes};
     constexpr int N = sizeof(to) / sizeof(to[0]);
     if (n != N + 3 || !PyType_Check(a[N + 2])) { PyErr_SetString(PyExc_TypeError, "bind: the addresses, two functions, a type"); return nullptr; }
     for (int i = 0; i < N; ++i) {

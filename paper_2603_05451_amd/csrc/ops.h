@@ -164,7 +164,21 @@ constexpr int weigh_key_blocks(int d_qk) { return d_qk <= 128 ? 2 : 1; }        
 constexpr int weigh_keys(int d_qk) { return 4 * 32 * weigh_key_blocks(d_qk); }  // of a block (of few rows: in one step)
 constexpr int weigh_rows(int d_qk) { return d_qk <= 128 ? 64 : 32; }            // of a tile of queries: 32 KiB of LDS at d = 128, twice
 constexpr int kWeighRound = 2 * 256;    // blocks that the chip holds
-inline int64_t weigh_units(int B, int Hkv, int d_qk, int64_t most) { return (int64_t)B * Hkv * ((most + weigh_keys(d_qk) - 1) / weigh_keys(d_qk)); }
+
+struct WeighShape {
+    bool split;         // the rows of a sequence may be divided over several blocks, whose sums are added by a second kernel
+    int64_t groups;     // of keys, at most
+    int64_t units;      // blocks' work: (group, share of the rows)s, at most
+};
+inline WeighShape weigh_shape(int B, int64_t T, int H, int Hkv, int d_qk, int64_t most)
+{
+    WeighShape s;
+    s.split = T * (H / Hkv) >= 512;
+    s.groups = (int64_t)B * Hkv * ((most + weigh_keys(d_qk) - 1) / weigh_keys(d_qk));
+    // (shares are made for a round of units, by an estimate of what each has to do that may be half of it)
+    s.units = s.groups + (s.split ? 2 * (kWeighRound + Hkv) : 0);
+    return s;
+}
 inline int weigh_blocks(int64_t units) { return (int)(units < 2 * kWeighRound ? units : 2 * kWeighRound); }
 
 // ---- eviction
@@ -250,6 +264,7 @@ struct CacheWeighArgs {
     int B, Nq, T, H;                    // T: rows of q in all
     float scale;
     int causal, fresh;
+    float* parts;               // sums of shares of the rows: [units][weigh_keys]
     bool f16;
     void* stream;
 };
