@@ -12,7 +12,7 @@ namespace {
 // ---- which rows and keys a block takes, from the boundaries and lengths in device memory
 struct ChunkPlanArgs {
     int B, T, G, Hkv, page_shift, most;     // most: keys that a row of the table has room for
-    int tile_keys, places;                  // keys of a step of the kernel for many rows; chunk_shape's places (0: no sequence's keys are divided)
+    int tile_shift, places;                 // keys of a step of the body for many rows, 2^tile_shift; blocks of a round per KV head (0: no keys are divided)
 };
 // A sequence: its first query, number of queries (0: there is nothing to do) and of keys.
 struct ChunkSeq {
@@ -25,7 +25,8 @@ struct ChunkPlace {
 };
 // Sequences with few rows (queries times heads of a group) go by another body: 32 rows to a block, 128 keys to a step of it.
 __device__ __forceinline__ bool chunk_few(const ChunkSeq& s, int G) { return s.nq * G <= kChunkFew; }
-__device__ __forceinline__ int chunk_rows(const ChunkSeq& s, int G) { return chunk_few(s, G) ? 32 : kChunkRows; }
+__device__ __forceinline__ int chunk_row_shift(const ChunkSeq& s, int G) { return chunk_few(s, G) ? 5 : 7; }        // rows of a block, 2^...
+static_assert(kChunkRows == 128);
 
 // What every wave of a launch finds out, a sequence per lane (the first 64 stay in registers).
 struct ChunkWork {
@@ -33,7 +34,7 @@ struct ChunkWork {
     const int* __restrict__ cu;
     const int* __restrict__ lens;
     ChunkSeq held;
-    int cost;               // of a part, in quarters of a step
+    float per_cost;         // 1 / (the cost of a part, in quarters of a step)
 
     __device__ __forceinline__ ChunkSeq fetch(int b) const { return fetch(p, cu, lens, b); }
     __device__ __forceinline__ static ChunkSeq fetch(const ChunkPlanArgs& p, const int* __restrict__ cu, const int* __restrict__ lens, int b)
@@ -52,15 +53,16 @@ struct ChunkWork {
         for (int b0 = 64; b0 < p.B; b0 += 64)
             if (f(fetch(b0 + lane), b0 + lane)) return;
     }
-    __device__ __forceinline__ int row_tiles(const ChunkSeq& s) const { const int n = chunk_rows(s, p.G); return (s.nq * p.G + n - 1) / n; }
-    __device__ __forceinline__ int step_keys(const ChunkSeq& s) const { return chunk_few(s, p.G) ? 128 : p.tile_keys; }
-    __device__ __forceinline__ int steps(const ChunkSeq& s) const { const int n = step_keys(s); return (s.len + n - 1) / n; }
+    __device__ __forceinline__ static int rounded(int x, int shift) { return (x + (1 << shift) - 1) >> shift; }
+    __device__ __forceinline__ int row_tiles(const ChunkSeq& s) const { return rounded(s.nq * p.G, chunk_row_shift(s, p.G)); }
+    __device__ __forceinline__ int step_shift(const ChunkSeq& s) const { return chunk_few(s, p.G) ? 7 : p.tile_shift; }
+    __device__ __forceinline__ int steps(const ChunkSeq& s) const { return rounded(s.len, step_shift(s)); }
     __device__ __forceinline__ int step_cost(const ChunkSeq& s) const { return chunk_few(s, p.G) ? kChunkFewCost : 4; }
+    // (by a product, not exactly rounded up: every wave that asks gets the same number, and the parts follow from it)
     __device__ __forceinline__ int parts(const ChunkSeq& s) const
     {
-        if (p.places == 0) return 1;
-        const int each = max(4, (cost + step_cost(s) - 1) / step_cost(s));     // a part has four steps or more
-        return max(1, (steps(s) + each - 1) / each);
+        const float of_cost = fminf(chunk_few(s, p.G) ? kChunkFewCost * per_cost : 4 * per_cost, 0.25f);      // a part has four steps or more
+        return p.places == 0 ? 1 : max(1, (int)ceilf((float)steps(s) * of_cost - 0.01f));
     }
     __device__ __forceinline__ int units(const ChunkSeq& s) const { return row_tiles(s) * parts(s); }
 
@@ -69,19 +71,17 @@ struct ChunkWork {
     __device__ __forceinline__ ChunkWork(const ChunkPlanArgs& plan, const int* __restrict__ c, const int* __restrict__ l) : p(plan), cu(c), lens(l)
     {
         held = fetch(threadIdx.x & 63);
-        cost = 1;
+        per_cost = 1.f;
         if (p.places == 0) return;
         float total = 0.f;
         each([&](const ChunkSeq& s, int) { total += (float)row_tiles(s) * (float)steps(s) * (float)step_cost(s); return false; });
-        total = wave_sum(total);
-        const int places = max(1, p.places / p.Hkv);
-        cost = (int)fminf(ceilf(total / (float)places), 1e9f);
+        per_cost = (float)p.places / fmaxf(wave_sum(total), 1.f);
         for (int i = 0; i < 3; ++i) {
             int n = 0;
             each([&](const ChunkSeq& s, int) { n += units(s); return false; });
             n = wave_sum(n);
-            if (n <= places) break;
-            cost += cost / 4 + 1;
+            if (n <= p.places) break;
+            per_cost *= 0.8f;
         }
     }
     // The sequence and its part that unit u is; false behind the last one.

@@ -134,7 +134,7 @@ inline int64_t cache_merge_blocks(const CacheShape& s, int B, int Nq, int H, int
 
 constexpr int kChunkRows = 128;         // rows (query, head of a KV head's group) of a block: 32 per wave
 constexpr int kChunkFew = 64;           // a sequence with no more rows goes by the body for few: 32 rows of a block, whose waves share the keys
-constexpr int kChunkFewCost = 2;        // a step of that body (128 keys), in quarters of a step of the other
+constexpr int kChunkFewCost = 3;        // a step of that body (128 keys), in quarters of a step of the other
 
 // Keys of a tile, and blocks that a CU holds: a tile of K and V in 16 bits, twice, is 64 KiB at d = 128 and at d = 256.
 constexpr int chunk_tile_keys(int d_qk) { return d_qk <= 128 ? 64 : 32; }
@@ -152,7 +152,7 @@ inline ChunkShape chunk_shape(int B, int T, int H, int Hkv, int d_qk, int64_t mo
     ChunkShape s{0, units};
     if (full * Hkv < round && most > (T * G > (int64_t)kChunkFew * B ? 512 : 1536)) {
         s.places = (int)round;
-        s.units = round / Hkv + 2 + units;
+        s.units = round / Hkv + 3 + units;
     }
     return s;
 }
