@@ -162,7 +162,7 @@ inline ChunkShape chunk_shape(int B, int T, int H, int Hkv, int d_qk, int64_t mo
 constexpr int kWeighFew = 32;           // a sequence with no more rows goes by the body for few
 constexpr int weigh_key_blocks(int d_qk) { return d_qk <= 128 ? 2 : 1; }        // of 32 keys that a wave takes together
 constexpr int weigh_keys(int d_qk) { return 4 * 32 * weigh_key_blocks(d_qk); }  // of a block (of few rows: in one step)
-constexpr int weigh_rows(int d_qk) { return d_qk <= 128 ? 64 : 32; }            // of a tile of queries: 32 KiB of LDS at d = 128, twice
+constexpr int weigh_rows(int d_qk) { return d_qk <= 64 ? 128 : 64; }            // of a tile of queries: 32 KiB of LDS at d = 128, twice
 constexpr int kWeighRound = 2 * 256;    // blocks that the chip holds
 
 struct WeighShape {
