@@ -90,6 +90,12 @@ def test_many_sequences_wide_table():
     _check(cache, w, t, lens, torch.randint(0, 150, (90,), generator=g).tolist(), 16)
 
 
+def test_lengths_beyond_the_table():
+    cache, w, t, lens = _case(7, [96, 64], 2, 64, 64, 4, 32)
+    lens[0], lens[1] = 2 ** 31 - 1, -7
+    _check(cache, w, t, lens, [50, 5], 9)
+
+
 def test_pages_outside_the_cache():
     """Their rows have the least weight; one that stays is NaN where it goes; nothing else changes."""
     import paper_2603_05451_amd as A
