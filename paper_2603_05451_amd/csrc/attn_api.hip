@@ -979,6 +979,6 @@ const char* attn_strerror(int code)
     }
 }
 
-int attn_version(void) { return 200; }
+int attn_version(void) { return 300; }
 
 }  // extern "C"
