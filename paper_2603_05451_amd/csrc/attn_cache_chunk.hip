@@ -12,6 +12,7 @@ namespace {
 // ---- which rows and keys a block takes, from the boundaries and lengths in device memory
 struct ChunkPlanArgs {
     int B, T, G, Hkv, page_shift, most;     // most: keys that a row of the table has room for
+    int few;                                // chunk_shape's
     int tile_shift, places;                 // keys of a step of the body for many rows, 2^tile_shift; blocks of a round per KV head (0: no keys are divided)
 };
 // A sequence: its first query, number of queries (0: there is nothing to do) and of keys.
@@ -24,8 +25,8 @@ struct ChunkPlace {
     int rt, part, parts, part_steps, unit;  // row tile; which of the parts of its keys, of so many steps; index of that part's unit
 };
 // Sequences with few rows (queries times heads of a group) go by another body: 32 rows to a block, 128 keys to a step of it.
-__device__ __forceinline__ bool chunk_few(const ChunkSeq& s, int G) { return s.nq * G <= kChunkFew; }
-__device__ __forceinline__ int chunk_row_shift(const ChunkSeq& s, int G) { return chunk_few(s, G) ? 5 : 7; }        // rows of a block, 2^...
+__device__ __forceinline__ bool chunk_few(const ChunkSeq& s, const ChunkPlanArgs& p) { return s.nq * p.G <= p.few; }
+__device__ __forceinline__ int chunk_row_shift(const ChunkSeq& s, const ChunkPlanArgs& p) { return chunk_few(s, p) ? 5 : 7; }        // rows of a block, 2^...
 static_assert(kChunkRows == 128);
 
 // What every wave of a launch finds out, a sequence per lane (the first 64 stay in registers).
@@ -35,6 +36,7 @@ struct ChunkWork {
     const int* __restrict__ lens;
     ChunkSeq held;
     float per_cost;         // 1 / (the cost of a part, in quarters of a step)
+    float per_unit;         // n0 steps of many rows take n0 / n + n / per_unit in n parts, which n^2 = n0 per_unit makes least
 
     __device__ __forceinline__ ChunkSeq fetch(int b) const { return fetch(p, cu, lens, b); }
     __device__ __forceinline__ static ChunkSeq fetch(const ChunkPlanArgs& p, const int* __restrict__ cu, const int* __restrict__ lens, int b)
@@ -54,15 +56,18 @@ struct ChunkWork {
             if (f(fetch(b0 + lane), b0 + lane)) return;
     }
     __device__ __forceinline__ static int rounded(int x, int shift) { return (x + (1 << shift) - 1) >> shift; }
-    __device__ __forceinline__ int row_tiles(const ChunkSeq& s) const { return rounded(s.nq * p.G, chunk_row_shift(s, p.G)); }
-    __device__ __forceinline__ int step_shift(const ChunkSeq& s) const { return chunk_few(s, p.G) ? 7 : p.tile_shift; }
+    __device__ __forceinline__ int row_tiles(const ChunkSeq& s) const { return rounded(s.nq * p.G, chunk_row_shift(s, p)); }
+    __device__ __forceinline__ int step_shift(const ChunkSeq& s) const { return chunk_few(s, p) ? 7 : p.tile_shift; }
     __device__ __forceinline__ int steps(const ChunkSeq& s) const { return rounded(s.len, step_shift(s)); }
-    __device__ __forceinline__ int step_cost(const ChunkSeq& s) const { return chunk_few(s, p.G) ? kChunkFewCost : 4; }
+    __device__ __forceinline__ int step_cost(const ChunkSeq& s) const { return chunk_few(s, p) ? kChunkFewCost : 4; }
     // (by a product, not exactly rounded up: every wave that asks gets the same number, and the parts follow from it)
     __device__ __forceinline__ int parts(const ChunkSeq& s) const
     {
-        const float of_cost = fminf(chunk_few(s, p.G) ? kChunkFewCost * per_cost : 4 * per_cost, 0.25f);      // a part has four steps or more
-        return p.places == 0 ? 1 : max(1, (int)ceilf((float)steps(s) * of_cost - 0.01f));
+        if (p.places == 0) return 1;
+        const bool few = chunk_few(s, p);
+        const float n = (float)steps(s), of_cost = fminf(few ? kChunkFewCost * per_cost : 4 * per_cost, 0.25f);      // a part has four steps or more
+        const int most = (int)ceilf(n * of_cost - 0.01f);
+        return max(1, few ? most : min(most, (int)__builtin_amdgcn_sqrtf(n * per_unit)));
     }
     __device__ __forceinline__ int units(const ChunkSeq& s) const { return row_tiles(s) * parts(s); }
 
@@ -71,10 +76,16 @@ struct ChunkWork {
     __device__ __forceinline__ ChunkWork(const ChunkPlanArgs& plan, const int* __restrict__ c, const int* __restrict__ l) : p(plan), cu(c), lens(l)
     {
         held = fetch(threadIdx.x & 63);
-        per_cost = 1.f;
+        per_cost = per_unit = 1.f;
         if (p.places == 0) return;
-        float total = 0.f;
-        each([&](const ChunkSeq& s, int) { total += (float)row_tiles(s) * (float)steps(s) * (float)step_cost(s); return false; });
+        float total = 0.f, many = 0.f;
+        each([&](const ChunkSeq& s, int) {
+            const float n = (float)row_tiles(s);
+            total += n * (float)steps(s) * (float)step_cost(s);
+            if (!chunk_few(s, p)) many += n;
+            return false;
+        });
+        per_unit = kChunkPartCost / fmaxf(wave_sum(many) * (float)p.Hkv, 1.f);
         per_cost = (float)p.places / fmaxf(wave_sum(total), 1.f);
         for (int i = 0; i < 3; ++i) {
             int n = 0;

@@ -133,26 +133,40 @@ inline int64_t cache_merge_blocks(const CacheShape& s, int B, int Nq, int H, int
 // ---- attention of chunks over the cache
 
 constexpr int kChunkRows = 128;         // rows (query, head of a KV head's group) of a block: 32 per wave
-constexpr int kChunkFew = 64;           // a sequence with no more rows goes by the body for few: 32 rows of a block, whose waves share the keys
-constexpr int kChunkFewCost = 3;        // a step of that body (128 keys), in quarters of a step of the other
+// A step of the body for few rows (128 keys), in quarters of a step of the other (26 sequences, 22 of them with one query, 100 ... 4096 keys,
+// G = 4, d = 128, 4 bits: 41.0, 36.3, 36.9 us with 2, 3, 4).
+constexpr int kChunkFewCost = 3;
+// So many parts of 128 rows cost what one step of the other does: each is 136 KB to memory and back (4 x 100 queries, 1000 keys, 8 heads:
+// 35.3 us with as many parts as there are places for, 28.9 so; 8 x 100: 42.0 and 33.8; 4 x 100, 2000 keys: 40.8 and 43.4).
+constexpr float kChunkPartCost = 53;
 
 // Keys of a tile, and blocks that a CU holds: a tile of K and V in 16 bits, twice, is 64 KiB at d = 128 and at d = 256.
 constexpr int chunk_tile_keys(int d_qk) { return d_qk <= 128 ? 64 : 32; }
 constexpr int chunk_blocks_per_cu(int d_qk) { return d_qk <= 192 ? 2 : 1; }
 
 struct ChunkShape {
+    int few;            // a sequence with no more rows goes by the body for few: 32 rows of a block, whose waves share the keys
     int places;         // blocks of one round if the keys of a row tile may be divided over several, else 0
     int64_t units;      // blocks per KV head at most: (row tile, part)s
 };
-// Whether keys are divided goes by the blocks that there are for sure without (T queries in full row tiles), and by the table's width.
+// Times below in us, G = 4, 8 KV heads, d = 128, 4 bits.
+// Few rows: shared keys are unpacked once per 32 rows rather than 128, but four waves have them each to itself.  Up to 64 rows (batch of 32,
+// 2000 keys: 48 rows 43.8 by the body for many, 36.0 by that for few; 64 rows 45.9, 37.2); up to 128 where row tiles leave most CUs idle (one
+// sequence of 4000 keys: 96 rows 21.2, 16.6; 128 rows 22.3, 17.7) but not in batches (32 of 2000 keys: 96 rows 53.3, 57.4; 128 rows 61.8, 66.3).
+// Keys are divided, which costs a merge, if the blocks that there are for sure without (T queries in full row tiles) do not fill a round
+// and the table is wide.  Undivided and divided: few rows, 8 sequences of 700 keys 10.0, 10.6; of 1000 12.1, 11.5; of 1400 17.4, 13.5; 32 of
+// 1400 keys 18.5, 19.6; of 2000 24.7, 23.0.  Many, 64 queries over 400 keys 17.2, 17.3; over 700 21.4, 19.2; 4 x 100 queries over 700 23.6,
+// 27.0; over 1000 28.8, 28.9; over 2000 more than 50, 43.4.
 inline ChunkShape chunk_shape(int B, int T, int H, int Hkv, int d_qk, int64_t most)
 {
     const int64_t G = H / Hkv, round = 256 * chunk_blocks_per_cu(d_qk);
-    const int64_t full = T * G / kChunkRows, units = full + 2 * (int64_t)(B < T ? B : T);
-    ChunkShape s{0, units};
-    if (full * Hkv < round && most > (T * G > (int64_t)kChunkFew * B ? 512 : 1536)) {
+    const int64_t full = T * G / kChunkRows, seqs = B < T ? B : T;
+    const bool idle = full * Hkv <= 64;
+    ChunkShape s{idle ? 128 : 64, 0, idle ? T * G / 32 + seqs : full + 2 * seqs};
+    const int64_t wide = T * G > (int64_t)s.few * B ? (idle ? 512 : 960) : ((int64_t)B * Hkv < 128 ? 960 : 1536);
+    if (full * Hkv < round && most > wide) {
         s.places = (int)round;
-        s.units = round / Hkv + 3 + units;
+        s.units += round / Hkv + 3;
     }
     return s;
 }

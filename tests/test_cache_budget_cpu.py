@@ -91,7 +91,7 @@ extern "C" {
 void t_chunk(int B, int T, int H, int Hkv, int d, long long most, long long* out)
 {
     const ChunkShape s = chunk_shape(B, T, H, Hkv, d, most);
-    out[0] = s.places; out[1] = s.units; out[2] = chunk_tile_keys(d); out[3] = kChunkFew; out[4] = kChunkFewCost;
+    out[0] = s.places; out[1] = s.units; out[2] = chunk_tile_keys(d); out[3] = s.few; out[4] = kChunkFewCost; out[5] = (long long)kChunkPartCost;
 }
 void t_weigh(int B, int T, int H, int Hkv, int d, long long most, long long* out)
 {
@@ -133,13 +133,17 @@ def test_chunk_units_fit_the_launch(shapes):
     r, f32 = random.Random(3), np.float32
     for B, T, nq, lens, most in _batches(r):
         Hkv, G, d = r.choice([1, 2, 8, 16]), r.choice([1, 3, 4, 8]), r.choice([64, 128, 192, 256])
-        places, room, keys, few_rows, few_cost = shapes("t_chunk", B, T, Hkv * G, Hkv, d, most)[:5]
+        places, room, keys, few_rows, few_cost, part_cost = shapes("t_chunk", B, T, Hkv * G, Hkv, d, most)[:6]
         seqs = []
         for n, m in zip(nq, lens):
             few = n * G <= few_rows
             step = 128 if few else keys
             seqs.append((-(-n * G // (32 if few else 128)), -(-m // step), few_cost if few else 4))
-        parts = lambda s, per: 1 if not places else max(1, math.ceil(float(f32(s[1]) * f32(min(f32(s[2]) * per, f32(0.25))) - f32(0.01))))
+        per_unit = f32(part_cost) / f32(max(sum(s[0] for s in seqs if s[2] == 4) * Hkv, 1))
+
+        def parts(s, per):
+            most_parts = math.ceil(float(f32(s[1]) * f32(min(f32(s[2]) * per, f32(0.25))) - f32(0.01)))
+            return 1 if not places else max(1, most_parts if s[2] != 4 else min(most_parts, int(math.sqrt(f32(s[1]) * per_unit))))
         per = f32(1)
         if places:
             mine = places // Hkv + 1

@@ -125,6 +125,22 @@ def test_boundaries_out_of_order():
     assert (o[10:] == 3).all()
 
 
+@pytest.mark.parametrize("fill", [0x7f, 0xff, 0x01, 0x00])
+def test_sequences_that_share_queries(fill):
+    """More work than T queries can have: some of it has no blocks.  What the workspace held before is not taken for where parts are, and only rows of
+    the sequences are written."""
+    import paper_2603_05451_amd as A
+    q, cache, t, _, _ = _case(9, [(40, 4000)], 2, 4, 64, 64, 4, 64, BF, pad=40)
+    cu = torch.tensor([0, 40] * 400 + [40, 70], dtype=torch.int32)          # every second sequence has none, for its boundaries descend
+    B = cu.numel() - 1
+    t, lens = t[:1].expand(B, -1).contiguous(), torch.full((B,), 4000, dtype=torch.int32)
+    n = A.attn_cache_chunk_workspace_bytes(cref.on_gpu(cache), B, 80, 8, t.shape[1])
+    ws = torch.full((n + 512,), fill, dtype=torch.uint8, device="cuda")
+    o, lse = torch.full((80, 8, 64), 3.0, dtype=BF, device="cuda"), torch.full((8, 80), 3.0, device="cuda")
+    _run(q, cache, t, cu, lens, 0.125, True, o=o, lse=lse, workspace=ws[:n])
+    assert n > 256 and (ws[n:] == fill).all() and (o[70:] == 3).all() and (lse[:, 70:] == 3).all()
+
+
 @pytest.mark.parametrize("bits,dtype", [(4, BF), (8, BF), (4, HF), (8, HF)])
 @pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (256, 256)])
 def test_numbers_that_are_not_finite(dqk, dv, bits, dtype):
