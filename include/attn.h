@@ -386,7 +386,7 @@ int attn_cache_weigh(int dtype, const attn_cache_t* cache, const void* q, const 
  * -0 and 0 are equal).  The cache is closed up in place, rows with their weights: with n = keep[b] - recent, survivors below n remain where they
  * are, the others go, in ascending order, to the places below n that are free, the recent rows, in order, to n ... keep[b] - 1.  So rows change
  * their places, which attention does not mind (keys hold their positions), and few rows are moved; the last ones remain in order.  What lies behind
- * the first keep[b] rows is left as it is, and its pages are free.  lens_out[b] = min(lens[b], keep[b]); lens_out may not be lens or keep.
+ * the first keep[b] rows is left as it is, and its pages are free.  lens_out[b] = min(lens[b], keep[b]); lens_out may not overlap lens or keep.
  *   - Lengths as in attn_cache_fwd.  A row of a page number outside the cache has the least weight; one that stays nevertheless is NaN, with weight 0, where
  *     it goes to a place in the cache.
  *   - Every row of the cache may belong to one sequence at most.

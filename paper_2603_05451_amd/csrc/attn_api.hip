@@ -876,7 +876,7 @@ int check_cache_weigh(const attn_cache_t* c, int B, int Nq, int H, int table_wid
     if (Nq <= 0) return ATTN_EINVAL;
     const int64_t T = packed ? Nq : (int64_t)B * Nq;
     if (T * H > 1 << 28 || T * H * c->d_qk > 1LL << 34) return ATTN_EUNSUPPORTED;
-    return attn::weigh_shape(B, T, H, c->Hkv, c->d_qk, (int64_t)table_width * c->page).units > 1 << 28 ? ATTN_EUNSUPPORTED : ATTN_OK;
+    return attn::weigh_shape(B, T, Nq, H, c->Hkv, c->d_qk, (int64_t)table_width * c->page).units > 1 << 28 ? ATTN_EUNSUPPORTED : ATTN_OK;
 }
 
 }  // namespace
@@ -884,7 +884,7 @@ int check_cache_weigh(const attn_cache_t* c, int B, int Nq, int H, int table_wid
 size_t attn_cache_weigh_workspace_bytes(const attn_cache_t* cache, int B, int Nq, int H, int table_width, int packed)
 {
     if (check_cache_weigh(cache, B, Nq, H, table_width, packed) != ATTN_OK) return 0;
-    const attn::WeighShape s = attn::weigh_shape(B, packed ? Nq : (int64_t)B * Nq, H, cache->Hkv, cache->d_qk, (int64_t)table_width * cache->page);
+    const attn::WeighShape s = attn::weigh_shape(B, packed ? Nq : (int64_t)B * Nq, Nq, H, cache->Hkv, cache->d_qk, (int64_t)table_width * cache->page);
     return s.split ? align_up((size_t)s.units * (size_t)attn::weigh_keys(cache->d_qk) * sizeof(float), 256) : 256;
 }
 
@@ -941,8 +941,10 @@ int attn_cache_evict(const attn_cache_t* cache, float* weights, const int* block
 {
     if (!weights || !block_table || !lens || !keep || !lens_out || !workspace) return ATTN_EINVAL;
     if (int rc = check_cache_table(cache, B, cache ? cache->Hkv : 0, table_width)) return rc;
-    if (recent < 0 || lens_out == lens || lens_out == keep) return ATTN_EINVAL;
+    if (recent < 0) return ATTN_EINVAL;
     if ((int64_t)B * cache->Hkv > attn::kMostBlocks || (int64_t)table_width * cache->page > 1 << 26) return ATTN_EUNSUPPORTED;
+    for (const int* in : {lens, keep})                     // (blocks of a sequence read them after another has written)
+        if (lens_out < in + B && in < lens_out + B) return ATTN_EINVAL;
     if (misaligned(cache->k_scale, 8) || misaligned(cache->v_scale, 8)) return ATTN_EINVAL;
     if (misaligned(weights, 16) || misaligned(block_table, 4) || misaligned(lens, 4) || misaligned(keep, 4) || misaligned(lens_out, 4) || misaligned(workspace, 256))
         return ATTN_EINVAL;

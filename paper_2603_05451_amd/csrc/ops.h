@@ -173,10 +173,14 @@ inline ChunkShape chunk_shape(int B, int T, int H, int Hkv, int d_qk, int64_t mo
 
 // ---- weights of cached keys
 
-constexpr int kWeighFew = 32;           // a sequence with no more rows goes by the body for few
+// A sequence with no more rows goes by the body for few, which has all of them in registers (32 sequences of 4000 keys, G = 4, 8 KV heads, d = 128, 4 bits:
+// one query 39.7 us by the body for many, 23.1 by that for few; 8 queries 45.1 and 24.2; one sequence with 8, 6.4 and 6.7).
+constexpr int kWeighFew = 32;
 constexpr int weigh_key_blocks(int d_qk) { return d_qk <= 128 ? 2 : 1; }        // of 32 keys that a wave takes together
 constexpr int weigh_keys(int d_qk) { return 4 * 32 * weigh_key_blocks(d_qk); }  // of a block (of few rows: in one step)
-constexpr int weigh_rows(int d_qk) { return d_qk <= 64 ? 128 : 64; }            // of a tile of queries: 32 KiB of LDS at d = 128, twice
+// Rows of a tile of queries: 16 KiB of LDS at d = 64 and 128, twice (1024 queries over 16 001 keys: d = 64 108 us with 64 rows, 104 with 128; d = 256 351
+// with 32 rows, 325 with 64).
+constexpr int weigh_rows(int d_qk) { return d_qk <= 64 ? 128 : 64; }
 constexpr int kWeighRound = 2 * 256;    // blocks that the chip holds
 
 struct WeighShape {
@@ -184,12 +188,15 @@ struct WeighShape {
     int64_t groups;     // of keys, at most
     int64_t units;      // blocks' work: (group, share of the rows)s, at most
 };
-inline WeighShape weigh_shape(int B, int64_t T, int H, int Hkv, int d_qk, int64_t most)
+// Rows are divided where a call has 256 and more, unless every sequence has few (Nq: queries that one may have), as the sum's launch is 3 us then
+// (32 x 4 queries over 4000 keys: 26.4 us with it, 23.6 without; 33 over 2000, 132 rows: 12.5, 11.1; 64 over 400 ... 2000: 12.3, 13.8; 128 over 2000: 13.2,
+// 23.1; 512 over 2000: 19.6, 58.8).
+inline WeighShape weigh_shape(int B, int64_t T, int64_t Nq, int H, int Hkv, int d_qk, int64_t most)
 {
     WeighShape s;
-    s.split = T * (H / Hkv) >= 512;
+    s.split = T * (H / Hkv) >= 256 && Nq * (H / Hkv) > kWeighFew;
     s.groups = (int64_t)B * Hkv * ((most + weigh_keys(d_qk) - 1) / weigh_keys(d_qk));
-    // (shares are made for a round of units, by an estimate of what each has to do that may be half of it)
+    // (shares are made for a round of units; rounding may make them one and a half)
     s.units = s.groups + (s.split ? 2 * (kWeighRound + Hkv) : 0);
     return s;
 }

@@ -63,7 +63,7 @@ def test_evict_refusals(L):  # noqa: F811
     def call(c=None, w=P, table=P, width=4, lens=P, keep=ctypes.c_void_p(0x2000), recent=3, B=3, out=ctypes.c_void_p(0x3000), ws=P, n=1 << 40):
         return L.attn_cache_evict(ctypes.byref(c or _cache()), w, table, width, lens, keep, recent, B, out, ws, n, None)
     _refused(call, [dict(w=None), dict(table=None), dict(lens=None), dict(keep=None), dict(out=None), dict(ws=None), dict(w=ODD), dict(lens=TWO), dict(keep=TWO), dict(out=TWO),
-                    dict(ws=WS), dict(width=0), dict(B=0), dict(recent=-1), dict(out=P), dict(out=ctypes.c_void_p(0x2000)), dict(n=256), dict(c=_cache(k_scale=0x1004)),
+                    dict(ws=WS), dict(width=0), dict(B=0), dict(recent=-1), dict(out=P), dict(out=ctypes.c_void_p(0x2000)), dict(out=ctypes.c_void_p(0x2008)), dict(out=ctypes.c_void_p(0x1ff8)), dict(n=256), dict(c=_cache(k_scale=0x1004)),
                     dict(c=_cache(v_scale=0x1001))],
              [dict(width=1 << 26), dict(width=1 << 22), dict(B=65537), dict(B=60000, c=_cache(Hkv=128))])
     size = lambda *a, **c: L.attn_cache_evict_workspace_bytes(ctypes.byref(_cache(**c)), *a)
@@ -95,7 +95,7 @@ void t_chunk(int B, int T, int H, int Hkv, int d, long long most, long long* out
 }
 void t_weigh(int B, int T, int H, int Hkv, int d, long long most, long long* out)
 {
-    const WeighShape s = weigh_shape(B, T, H, Hkv, d, most);
+    const WeighShape s = weigh_shape(B, T, T, H, Hkv, d, most);
     out[0] = s.split; out[1] = s.groups; out[2] = s.units; out[3] = weigh_keys(d); out[4] = weigh_rows(d); out[5] = kWeighFew; out[6] = kWeighRound;
 }
 }
@@ -162,14 +162,14 @@ def test_weigh_units_fit_the_launch(shapes):
     """The same of the shares of rows that keys are weighed by."""
     r, f32 = random.Random(4), np.float32
     for B, T, nq, lens, most in _batches(r):
-        Hkv, G, d, causal = r.choice([1, 2, 8, 16]), r.choice([1, 3, 4, 8]), r.choice([64, 128, 192, 256]), r.random() < 0.5
+        Hkv, G, d = r.choice([1, 2, 8, 16]), r.choice([1, 3, 4, 8]), r.choice([64, 128, 192, 256])
         split, groups, room, keys, rows, few_rows, round_ = shapes("t_weigh", B, T, Hkv * G, Hkv, d, most)[:7]
         steps = [-(-m // keys) if n else 0 for n, m in zip(nq, lens)]
         few, tiles = [n * G <= few_rows for n in nq], [-(-n * G // rows) for n in nq]
         of_few = sum(s for s, f in zip(steps, few) if f)
-        of_many = sum(s * t * (1 - 0.5 * min(1, n / m) if causal and m else 1) for s, t, f, n, m in zip(steps, tiles, few, nq, lens) if not f)
+        of_many = sum(s * t for s, t, f in zip(steps, tiles, few) if not f)
         few_steps = max(1, math.ceil(f32(of_few) * f32(Hkv) / f32(round_)))
-        share = max(4, math.ceil(f32(of_many) * f32(Hkv) / f32(round_))) if split else 1 << 30
+        share = max(2, math.ceil(f32(of_many) * f32(Hkv) / f32(round_))) if split else 1 << 30
         units = kinds = 0
         for s, t, f in zip(steps, tiles, few):
             g = -(-s // (few_steps if f else 1))
