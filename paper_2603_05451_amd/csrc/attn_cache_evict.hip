@@ -7,6 +7,9 @@
 // order, by sums over the block, and the i-th mover goes into the i-th hole.  At most len - left + recent rows are moved at all, where closing
 // the cache up in order would move nearly all of them.  The recent rows then go to the places from `stay` on, in order.
 //
+// What bounds it: for some thousand rows and many heads (32 sequences of 4352 rows, 8 heads: 11.9 us, 5.1 for the bytes) a chain of fixed parts, and in a
+// block of 16 waves the vector instructions' turns; for one long sequence (30 001 rows: 29 us) those of the eight blocks that there are.
+//
 // The only atomics are counts of whole numbers: results do not depend on their order.
 #include "common.h"
 #include "launch.h"
@@ -22,6 +25,7 @@ struct EvictPlan {
 };
 
 constexpr int NT = 1024;            // (512 are slower from some thousand rows on, 4352 rows 13.7 and 11.3 us, and no faster for few)
+constexpr int kCopies = 2;           // of the histogram, a lane's the even or the odd one (30 001 rows: 30.8 us with one, 29.8 with two, 29.9 with four)
 constexpr int kAtOnce = 4;          // 16-byte pieces of rows that a thread moves in a turn
 
 // Weights in ascending order as whole numbers: 0 is a row that is not in the cache, NaN the greatest, -0 and 0 are equal.
@@ -77,7 +81,7 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
     constexpr int KROW = DQK * BITS / 8, VROW = DV * BITS / 8;
     // weights of up to plan.held keys as whole numbers, and later the list of places: an entry lies no further than its key's number
     extern __shared__ __attribute__((aligned(16))) uint32_t held_[];
-    __shared__ int count[2048];
+    __shared__ __attribute__((aligned(16))) int count[2048][kCopies];
     __shared__ int part_[4][NT / 64];
     __shared__ int found[3];
     ATTN_LDS uint32_t* const held = (ATTN_LDS uint32_t*)held_;
@@ -124,7 +128,9 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
         while (low > 0) {
             const int bits = min(low, 11);
             low -= bits;
-            for (int i = tid; i < 2048; i += NT) count[i] = 0;
+            for (int i = tid; i < 2048; i += NT)
+#pragma unroll
+                for (int c = 0; c < kCopies; ++c) count[i][c] = 0;
             __syncthreads();
 #pragma unroll 1
             for (int j = 4 * tid; j < of; j += 4 * NT) {
@@ -132,7 +138,7 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
                 int at[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint64_t begins = (uint64_t)x[e] >> low;                     // (low + bits may be 32)
+                    const uint32_t begins = x[e] >> low;
                     at[e] = j + e < of && begins >> bits == prefix ? (int)(begins & ((1u << bits) - 1)) : -1;
                 }
                 // (equal ones in one go: lanes that add to one place do so one after the other)
@@ -140,7 +146,7 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const bool more = e < 3 && at[e] == at[e < 3 ? e + 1 : 3];
-                    if (!more && at[e] >= 0) atomicAdd(&count[at[e]], n);
+                    if (!more && at[e] >= 0) atomicAdd(&count[at[e]][tid % kCopies], n);
                     n = more ? n + 1 : 1;
                 }
             }
@@ -149,7 +155,12 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
             constexpr int PER = 2048 / NT;
             int here[PER], sum = 0, before, all;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) sum += here[i] = count[2047 - PER * tid - i];
+            for (int i = 0; i < PER; ++i) {
+                here[i] = 0;
+#pragma unroll
+                for (int c = 0; c < kCopies; ++c) here[i] += count[2047 - PER * tid - i][c];
+                sum += here[i];
+            }
             block_sums(sum, part(0), before, all);
             if (before < wanted && wanted <= before + sum) {
 #pragma unroll
