@@ -77,6 +77,14 @@ def test_weights_in_order(kind):
         _check(cache, w, t, lens, [keep], recent)
 
 
+@pytest.mark.parametrize("of", [4096, 4097, 8191, 8192, 8193, 8197, 20001])
+def test_ties_over_turns(of):
+    """Rows that go are the last of those that are equal, zeros all over the sequence; turns of 4096 and of 8192 keys, and one more or less."""
+    cache, w, t, lens = _case(of, [of + 5], 1, 64, 64, 4, 64)
+    zeros = int((w[t[0, torch.arange(of) // 64].long(), 0, torch.arange(of) % 64] == 0).sum())
+    _check(cache, w, t, lens, [of + 5 - zeros // 2], 5)
+
+
 def test_long_sequence():
     cache, w, t, lens = _case(5, [70001], 1, 64, 64, 4, 256)
     _check(cache, w, t, lens, [20000], 300)
