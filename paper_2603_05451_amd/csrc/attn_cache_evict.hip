@@ -7,8 +7,8 @@
 // order, by sums over the block, and the i-th mover goes into the i-th hole.  At most len - left + recent rows are moved at all, where closing
 // the cache up in order would move nearly all of them.  The recent rows then go to the places from `stay` on, in order.
 //
-// What bounds it: for some thousand rows and many heads (32 sequences of 4352 rows, 8 heads: 11.9 us, 5.1 for the bytes) a chain of fixed parts, and in a
-// block of 16 waves the vector instructions' turns; for one long sequence (30 001 rows: 29 us) those of the eight blocks that there are.
+// What bounds it: for some thousand rows and many heads (32 sequences of 4352 rows, 8 heads: 10.3 us, 5.1 for the bytes) a chain of fixed parts, and in a
+// block of 16 waves the vector instructions' turns; for one long sequence (30 001 rows: 26 us) those of the eight blocks that there are.
 //
 // The only atomics are counts of whole numbers: results do not depend on their order.
 #include "common.h"
