@@ -68,6 +68,15 @@ def test_long_keys_divided(dqk, dv, bits):
     cref.check_attention(q, cache, t, cu, lens, dqk ** -0.5, True, o.cpu(), lse.cpu(), bits)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dqk,dv,bits", [(64, 64, 8), (96, 96, 4), (192, 128, 4), (256, 256, 8)])
+def test_few_rows_divided(dqk, dv, bits, causal):
+    """Up to 128 rows, whose keys are divided, next to one that has more, one without keys and one without queries."""
+    q, cache, t, cu, lens = _case(dqk, [(25, 3000), (17, 1500), (32, 2049), (1, 2500), (33, 1100), (5, 0), (0, 900), (16, 31)], 2, 4, dqk, dv, bits, 32, BF)
+    o, lse = _run(q, cache, t, cu, lens, dqk ** -0.5, causal)
+    cref.check_attention(q, cache, t, cu, lens, dqk ** -0.5, causal, o.cpu(), lse.cpu(), bits)
+
+
 def test_many_sequences():
     """More than a wave has lanes, some without queries, some without keys, lengths beyond the table and negative ones."""
     g = cref.gen(5)
