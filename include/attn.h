@@ -370,8 +370,9 @@ int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, co
  * Nq is T, lse [H, T]), with cu_seqlens null those of attn_cache_fwd (q [B, Nq, H, d_qk], lse [B, H, Nq]).
  *   - fresh != 0: the sequence's last keys, as many as it has queries, are the call's own: their weights are set, not added to, so that
  *     what a page held before does not matter.
- *   - A query with lse = -inf (it saw no key) adds nothing.  A key that is not finite has the weight NaN.  Entries of the table that are
- *     outside the cache are passed over.  Weights of other rows are not touched.
+ *   - A query with lse = -inf (it saw no key, or the caller leaves it out so) adds nothing to finite keys, whatever its row of q holds.  Entries of the
+ *     table that are outside the cache are passed over.  Weights of other rows are not touched.
+ *   - A key that is not finite has the weight NaN.
  *   - Every row of the cache may belong to one sequence at most (a page that two sequences share has unspecified weights).
  *   - Sums are in fp32, in an order that depends on the sizes and lengths alone.  Limits as in the two calls.
  *   workspace: attn_cache_weigh_workspace_bytes(...) bytes (packed: whether there are cu_seqlens), 256-byte aligned, contents ignored.  One kernel, and
