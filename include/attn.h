@@ -372,7 +372,9 @@ int attn_cache_chunk_fwd(int dtype, const attn_cache_t* cache, const void* q, co
  *     what a page held before does not matter.
  *   - A query with lse = -inf (it saw no key, or the caller leaves it out so) adds nothing to finite keys, whatever its row of q holds.  Entries of the
  *     table that are outside the cache are passed over.  Weights of other rows are not touched.
- *   - A key that is not finite has the weight NaN.
+ *   - Numbers that are not finite go by the formula: a NaN key has the weight NaN, and so has every key that a query with lse = NaN sees; the queries
+ *     that see a NaN key have that lse from the attention calls.  (attn_cache_evict takes NaN for the greatest.)  An infinite key (fp16: one beyond
+ *     its range) gets 0 from a score of -inf, NaN from one of +inf or from a query left out.
  *   - Every row of the cache may belong to one sequence at most (a page that two sequences share has unspecified weights).
  *   - Sums are in fp32, in an order that depends on the sizes and lengths alone.  Limits as in the two calls.
  *   workspace: attn_cache_weigh_workspace_bytes(...) bytes (packed: whether there are cu_seqlens), 256-byte aligned, contents ignored.  One kernel, and
