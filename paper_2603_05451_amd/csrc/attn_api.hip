@@ -885,7 +885,7 @@ size_t attn_cache_weigh_workspace_bytes(const attn_cache_t* cache, int B, int Nq
 {
     if (check_cache_weigh(cache, B, Nq, H, table_width, packed) != ATTN_OK) return 0;
     const attn::WeighShape s = attn::weigh_shape(B, packed ? Nq : (int64_t)B * Nq, Nq, H, cache->Hkv, cache->d_qk, (int64_t)table_width * cache->page);
-    return s.split ? align_up((size_t)s.units * (size_t)attn::weigh_keys(cache->d_qk) * sizeof(float), 256) : 256;
+    return s.split ? align_up((size_t)s.parts * (size_t)attn::weigh_keys(cache->d_qk) * sizeof(float), 256) : 256;
 }
 
 int attn_cache_weigh(int dtype, const attn_cache_t* cache, const void* q, const attn_strides_t* sq, const float* lse, float* weights,

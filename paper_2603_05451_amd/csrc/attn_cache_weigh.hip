@@ -67,14 +67,16 @@ struct WeighWork {
     }
     __device__ __forceinline__ int groups(const WeighSeq& s) const { const int n = few(s) ? few_steps : 1; return (steps(s) + n - 1) / n; }
     __device__ __forceinline__ int shares(const WeighSeq& s) const { return few(s) ? 1 : max(1, (int)(((int64_t)tiles(s) + share_tiles / 2) / share_tiles)); }
-    // Group (ALL: and share) number u of all sequences'; false behind the last one.  Unit: the first of its sequence's units.
+    // Group (ALL: and share) number u of all sequences'; false behind the last one.  Part: where the sums of its sequence's (share, group)s begin, if there
+    // are more shares than one.
     template <bool ALL>
-    __device__ __forceinline__ bool find(int u, WeighPlace& at, int& unit) const
+    __device__ __forceinline__ bool find(int u, WeighPlace& at, int& part) const
     {
-        unit = 0;
+        part = 0;
         for (int b0 = 0; b0 < p.B; b0 += 64) {
             const WeighSeq s = seq(b0);
-            const int g = groups(s), n = shares(s), mine = ALL ? g * n : g, upto = wave_prefix(mine), units = ALL ? upto : wave_prefix(g * n);
+            const int g = groups(s), n = shares(s), mine = ALL ? g * n : g, upto = wave_prefix(mine);
+            const int divided = n > 1 ? g * n : 0, parts = p.split ? wave_prefix(divided) : 0;
             const uint64_t past = __ballot(upto > u);
             if (past) {
                 const int l = __builtin_ctzll(past);
@@ -88,11 +90,11 @@ struct WeighWork {
                 at.group = ALL ? local - at.share * at.groups : local;
                 at.group_keys = KEYS * ((of(steps(s)) + at.groups - 1) / at.groups);
                 at.share_tiles = (of(tiles(s)) + at.shares - 1) / at.shares;
-                unit += of(units) - of(g * n);
+                part += of(parts) - of(divided);
                 return true;
             }
             u -= __builtin_amdgcn_readlane(upto, 63);
-            unit += __builtin_amdgcn_readlane(units, 63);
+            part += __builtin_amdgcn_readlane(parts, 63);
         }
         return false;
     }

@@ -187,6 +187,7 @@ struct WeighShape {
     bool split;         // the rows of a sequence may be divided over several blocks, whose sums are added by a second kernel
     int64_t groups;     // of keys, at most
     int64_t units;      // blocks' work: (group, share of the rows)s, at most
+    int64_t parts;      // those of sequences whose rows are divided, whose sums go by the workspace, at most
 };
 // Rows are divided where a call has 256 and more, unless every sequence has few (Nq: queries that one may have), as the sum's launch is 3 us then
 // (32 x 4 queries over 4000 keys: 26.4 us with it, 23.6 without; 33 over 2000, 132 rows: 12.5, 11.1; 64 over 400 ... 2000: 12.3, 13.8; 128 over 2000: 13.2,
@@ -198,6 +199,8 @@ inline WeighShape weigh_shape(int B, int64_t T, int64_t Nq, int H, int Hkv, int 
     s.groups = (int64_t)B * Hkv * ((most + weigh_keys(d_qk) - 1) / weigh_keys(d_qk));
     // (shares are made for a round of units; rounding may make them one and a half)
     s.units = s.groups + (s.split ? 2 * (kWeighRound + Hkv) : 0);
+    // (n of 2 and more that were rounded from x are 4/3 x at most, and all x are a round: 683)
+    s.parts = !s.split ? 0 : s.units < kWeighRound * 3 / 2 ? s.units : kWeighRound * 3 / 2;
     return s;
 }
 inline int weigh_blocks(int64_t units) { return (int)(units < 2 * kWeighRound ? units : 2 * kWeighRound); }
@@ -285,7 +288,7 @@ struct CacheWeighArgs {
     int B, Nq, T, H;                    // T: rows of q in all
     float scale;
     int causal, fresh;
-    float* parts;               // sums of shares of the rows: [units][weigh_keys]
+    float* parts;               // sums of shares of the rows: [weigh_shape's parts][weigh_keys]
     bool f16;
     void* stream;
 };
