@@ -805,12 +805,12 @@ int check_cache_chunk(const attn_cache_t* c, int B, int T, int H, int table_widt
     return s.places && (int64_t)T * ((H + per - 1) / per) > attn::kMostBlocks ? ATTN_EUNSUPPORTED : ATTN_OK;
 }
 
-// partial results of every block, if there may be more than one to a row tile: O | maximum and sum | where a sequence's parts are
+// results of parts, if there may be more than one to a row tile: O | maximum and sum | where a sequence's parts are
 CacheParts chunk_parts(const attn_cache_t* c, int B, int T, int H, int table_width)
 {
     const attn::ChunkShape s = attn::chunk_shape(B, T, H, c->Hkv, c->d_qk, (int64_t)table_width * c->page);
     if (s.places == 0) return {0, 0, 256};
-    const size_t rows = (size_t)s.units * (size_t)c->Hkv * attn::kChunkRows;
+    const size_t rows = (size_t)s.part_tiles * (size_t)c->Hkv * 32;
     CacheParts w;
     w.ml_off = align_up(rows * c->d_v * sizeof(float), 256);
     w.merge_off = w.ml_off + align_up(rows * 2 * sizeof(float), 256);

@@ -22,7 +22,8 @@ struct ChunkSeq {
 struct ChunkPlace {
     ChunkSeq s;
     int b;                                  // its index
-    int rt, part, parts, part_steps, unit;  // row tile; which of the parts of its keys, of so many steps; index of that part's unit
+    int rt, part, parts, part_steps;        // row tile; which of the parts of its keys, of so many steps
+    int first_tile, tile;                   // where results of parts go, in tiles of 32 rows per KV head: the sequence's first, the unit's first
 };
 // Sequences with few rows (queries times heads of a group) go by another body: 32 rows to a block, 128 keys to a step of it.
 __device__ __forceinline__ bool chunk_few(const ChunkSeq& s, const ChunkPlanArgs& p) { return s.nq * p.G <= p.few; }
@@ -70,6 +71,7 @@ struct ChunkWork {
         return max(1, few ? most : min(most, (int)__builtin_amdgcn_sqrtf(n * per_unit)));
     }
     __device__ __forceinline__ int units(const ChunkSeq& s) const { return row_tiles(s) * parts(s); }
+    __device__ __forceinline__ int unit_tiles(const ChunkSeq& s) const { return 1 << (chunk_row_shift(s, p) - 5); }      // tiles of 32 rows of a unit
 
     // What a part costs: all steps of all row tiles in about `places` parts (a round of blocks), longer if the sequences' last, shorter parts
     // would make it more.
@@ -99,20 +101,23 @@ struct ChunkWork {
     __device__ __forceinline__ bool find(int u, ChunkPlace& at) const
     {
         bool found = false;
-        int before = 0;
+        int before = 0, tiles_before = 0;
         each([&](const ChunkSeq& s, int b) {
             const int mine = units(s), upto = before + wave_prefix(mine);
+            const int tiles = p.places && parts(s) > 1 ? mine * unit_tiles(s) : 0;
+            const int tiles_upto = p.places ? tiles_before + wave_prefix(tiles) : 0;
             const uint64_t past = __ballot(upto > u);
             if (past) {
                 const int l = __builtin_ctzll(past);
                 auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
                 at.s = {of(s.q0), of(s.nq), of(s.len)};
                 at.b = of(b);
+                at.first_tile = of(tiles_upto) - of(tiles);
                 place(at, u - (of(upto) - of(mine)));
-                at.unit = u;
                 return found = true;
             }
             before = __builtin_amdgcn_readlane(upto, 63);
+            tiles_before = __builtin_amdgcn_readlane(tiles_upto, 63);
             return false;
         });
         return found;
@@ -126,6 +131,7 @@ struct ChunkWork {
         at.part = local / rts;
         at.rt = rts - 1 - (local - at.part * rts);
         at.part_steps = (n + at.parts - 1) / at.parts;
+        at.tile = at.first_tile + local * unit_tiles(at.s);
     }
     // The sequence of query t, as its lengths say (what its parts are, the attention kernel has left behind).
     __device__ __forceinline__ static bool of_query(const ChunkPlanArgs& p, const int* __restrict__ cu, const int* __restrict__ lens, int t, ChunkSeq& s, int& b)

@@ -148,7 +148,9 @@ struct ChunkShape {
     int few;            // a sequence with no more rows goes by the body for few: 32 rows of a block, whose waves share the keys
     int places;         // blocks of one round if the keys of a row tile may be divided over several, else 0
     int64_t units;      // blocks per KV head at most: (row tile, part)s
+    int64_t part_tiles; // room for results of parts, per KV head: 32 rows (a part of a row tile of many rows has four)
 };
+inline int chunk_places(int places, int Hkv) { return places ? places / Hkv + 1 : 0; }        // per KV head
 // Times below in us, G = 4, 8 KV heads, d = 128, 4 bits.
 // Few rows: shared keys are unpacked once per 32 rows rather than 128, but four waves have them each to itself.  Up to 64 rows (batch of 32,
 // 2000 keys: 48 rows 43.8 by the body for many, 36.0 by that for few; 64 rows 45.9, 37.2); up to 128 where row tiles leave most CUs idle (one
@@ -162,11 +164,14 @@ inline ChunkShape chunk_shape(int B, int T, int H, int Hkv, int d_qk, int64_t mo
     const int64_t G = H / Hkv, round = 256 * chunk_blocks_per_cu(d_qk);
     const int64_t full = T * G / kChunkRows, seqs = B < T ? B : T;
     const bool idle = full * Hkv <= 64;
-    ChunkShape s{idle ? 128 : 64, 0, idle ? T * G / 32 + seqs : full + 2 * seqs};
+    ChunkShape s{idle ? 128 : 64, 0, idle ? T * G / 32 + seqs : full + 2 * seqs, 0};
     const int64_t wide = T * G > (int64_t)s.few * B ? (idle ? 512 : 960) : ((int64_t)B * Hkv < 128 ? 960 : 1536);
     if (full * Hkv < round && most > wide) {
         s.places = (int)round;
         s.units += round / Hkv + 3;
+        // Only what is divided has results of parts.  n parts of 2 and more, rounded up from x > 1, are fewer than 2 x, and all x are the places.
+        const int64_t divided = 2 * chunk_places(s.places, Hkv);
+        s.part_tiles = (s.units < divided ? s.units : divided) * (T * G > s.few ? kChunkRows / 32 : 1);
     }
     return s;
 }
@@ -316,7 +321,7 @@ struct CacheChunkArgs {
     int B, T, H;
     float scale;
     int causal;
-    float *part_o, *part_ml;    // unnormalised results of parts: [units * Hkv][kChunkRows][d_v], and {maximum, sum} of each row
+    float *part_o, *part_ml;    // unnormalised results of parts: [part_tiles * Hkv][32][d_v], and {maximum, sum} of each row
     int* merge;                 // [B][4]: where a sequence's parts are
     bool f16;
     void* stream;
