@@ -394,7 +394,8 @@ int attn_cache_weigh(int dtype, const attn_cache_t* cache, const void* q, const 
  *     it goes to a place in the cache.
  *   - Every row of the cache may belong to one sequence at most.
  *   - k_scale and v_scale are 8-byte aligned.  B * Hkv is 2^22 at most, table_width * page 2^26.
- *   workspace: attn_cache_evict_workspace_bytes(...) bytes (4 for every row that the table has room for, and head), 256-byte aligned, contents ignored. */
+ *   workspace: attn_cache_evict_workspace_bytes(...) bytes (4 for every row that the table has room for, and head; 64 KiB at most for tables of up to
+ *   32 768 rows), 256-byte aligned, contents ignored. */
 size_t attn_cache_evict_workspace_bytes(const attn_cache_t* cache, int B, int table_width);
 int attn_cache_evict(const attn_cache_t* cache, float* weights, const int* block_table, int table_width, const int* lens, const int* keep, int recent,
                      int B, int* lens_out, void* workspace, size_t workspace_bytes, void* stream);

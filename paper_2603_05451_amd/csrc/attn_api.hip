@@ -933,7 +933,7 @@ size_t attn_cache_evict_workspace_bytes(const attn_cache_t* cache, int B, int ta
     if (check_cache_table(cache, B, cache ? cache->Hkv : 0, table_width) != ATTN_OK || (int64_t)B * cache->Hkv > attn::kMostBlocks ||
         (int64_t)table_width * cache->page > 1 << 26)
         return 0;
-    return align_up((size_t)B * (size_t)cache->Hkv * (size_t)attn::evict_ints((int64_t)table_width * cache->page) * sizeof(int), 256);
+    return align_up((size_t)attn::evict_bytes((int64_t)B * cache->Hkv, (int64_t)table_width * cache->page), 256);
 }
 
 int attn_cache_evict(const attn_cache_t* cache, float* weights, const int* block_table, int table_width, const int* lens, const int* keep, int recent,

@@ -295,12 +295,11 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
 template <int DQK, int DV, int BITS>
 static int cache_evict_b(const CacheEvictArgs& a)
 {
-    constexpr int room = 32768;                            // keys: 128 KiB
-    const int most = a.table_width << a.c.page_shift, held = ((most < room ? most : room) + 3) & ~3;
+    const int most = a.table_width << a.c.page_shift, held = ((most < kEvictHeld ? most : kEvictHeld) + 3) & ~3;
     const EvictPlan plan{a.c.Hkv, a.c.page_shift, most, a.table_width, a.c.pages, a.recent, held, evict_ints(most)};
     auto kern = attn_cache_evict_kernel<DQK, DV, BITS>;
     static LdsOptIn lds;
-    if (!lds.allow(kern, 4 * room)) return -3;
+    if (!lds.allow(kern, 4 * kEvictHeld)) return -3;
     return launch_kernel(kern, dim3((unsigned)(a.B * a.c.Hkv)), dim3(NT), (size_t)(4 * held), a.stream, (uint8_t*)a.c.k, (uint8_t*)a.c.k_scale, (uint8_t*)a.c.v,
                          (uint8_t*)a.c.v_scale, a.weights, a.table, a.lens, a.keep, a.lens_out, plan, a.places) == hipSuccess ? 0 : -3;
 }

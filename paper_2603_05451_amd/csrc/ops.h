@@ -212,7 +212,14 @@ inline int weigh_blocks(int64_t units) { return (int)(units < 2 * kWeighRound ? 
 
 // ---- eviction
 
+constexpr int kEvictHeld = 32768;       // keys whose weights, and lists of places, a block has in LDS: 128 KiB
 inline int64_t evict_ints(int64_t most) { return (most + 3) / 4 * 4; }     // of a (sequence, KV head)'s list of places
+// Lists of wider tables go by the workspace.  Where no sequence can have one there it is not touched, and is what the lists would take only as long as that is little.
+inline int64_t evict_bytes(int64_t heads, int64_t most)
+{
+    const int64_t lists = heads * evict_ints(most) * 4;
+    return most <= kEvictHeld && lists > 65536 ? 65536 : lists;
+}
 
 }  // namespace attn
 
@@ -305,7 +312,7 @@ struct CacheEvictArgs {
     const int *table, *lens, *keep;
     int* lens_out;
     int table_width, B, recent;
-    int* places;                // [B][Hkv][evict_ints(most)]
+    int* places;                // [B][Hkv][evict_ints(most)], used where most is beyond kEvictHeld
     void* stream;
 };
 int launch_cache_evict(const CacheEvictArgs& a);

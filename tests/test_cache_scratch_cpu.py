@@ -130,3 +130,12 @@ def test_chunk_sizes(L):  # noqa: F811
         for width in (64, 512):
             assert size(B, B, width) <= 66 * 2 * 8 * 128 * (128 + 2) * 4 + 16 * B + 1024
     assert size(1, 2048, 512) <= 70 * MIB and size(1, 1 << 14, 512) == 256
+
+
+def test_evict_sizes(L):  # noqa: F811
+    """Tables of up to 32 768 rows, whose lists are in LDS, ask for 64 KiB at most; wider ones for every row."""
+    size = lambda B, width, **c: L.attn_cache_evict_workspace_bytes(ctypes.byref(_cache(**{**dict(Hkv=8, page=64, pages=1 << 19), **c})), B, width)
+    for B in (1, 64, 1024, 65536):
+        for width in (1, 64, 512):
+            assert size(B, width) == min(B * 8 * width * 64 * 4, 65536)
+        assert size(B, 513) == B * 8 * 513 * 64 * 4
