@@ -352,6 +352,9 @@ int attn_cache_fwd(int dtype, const attn_cache_t* cache, const void* q, const at
  * cached before and the chunk itself, already written.  q and o are views [T, H, d] as in attn_rope_fwd (`batch` is not used), lse [H, T]
  * contiguous.  causal != 0: a sequence's last query is aligned with its last key (key j visible to its query i iff j <= i + lens[b] - queries).
  *   - Empty queries, lengths, pages and numbers that are not finite are dealt with as in attn_cache_fwd, whatever the chunk's length.
+ *   - exp(score - maximum) is rounded to the element type for its product with V, as in the other attention calls (its sum, and lse, are of what was not
+ *     rounded); all sums are in fp32, and o is rounded once.  The two roundings are of one size: of normal numbers o is off by 2.3e-3 relative in
+ *     bf16, 2.8e-4 in fp16, where that of o alone makes 1.7e-3 and 2.1e-4.
  *   - A sequence whose boundaries do not ascend within 0 ... T has no queries.  Rows of q that belong to no sequence (padding behind the last
  *     one) are not touched in o and lse.  Two sequences must not share queries (the results of such rows are unspecified).
  *   - Boundaries, lengths and pages are read on the device: a captured call may be replayed with others.

@@ -7,8 +7,10 @@
 // order, by sums over the block, and the i-th mover goes into the i-th hole.  At most len - left + recent rows are moved at all, where closing
 // the cache up in order would move nearly all of them.  The recent rows then go to the places from `stay` on, in order.
 //
-// What bounds it: for some thousand rows and many heads (32 sequences of 4352 rows, 8 heads: 10.3 us, 5.1 for the bytes) a chain of fixed parts, and in a
-// block of 16 waves the vector instructions' turns; for one long sequence (30 001 rows: 26 us) those of the eight blocks that there are.
+// What bounds it (8 heads, d = 128, 4 bits; states that were not evicted before, their memory not in the caches): for some thousand rows and many heads (32
+// sequences of 4352 rows to 4096: 21.5 us, 5.1 for the bytes) a chain of fixed parts, each a latency of LDS or memory, and in a block of 16 waves the vector
+// instructions' turns; for one long sequence (30 001 rows to 4096: 71 us) the eight blocks that there are: 26 us of selection, as a pass over the same state
+// takes that finds nearly all survivors in place, and the moves of 3500 rows of each head through one CU.
 //
 // The only atomics are counts of whole numbers: results do not depend on their order.
 #include "common.h"
@@ -24,8 +26,12 @@ struct EvictPlan {
     int64_t ints;
 };
 
-constexpr int NT = 1024;            // (512 are slower from some thousand rows on, 4352 rows 13.7 and 11.3 us, and no faster for few)
-constexpr int kCopies = 2;           // of the histogram, a lane's the even or the odd one (30 001 rows: 30.8 us with one, 29.8 with two, 29.9 with four)
+// (512 are slower where blocks are few, 32 sequences of 4352 rows 25 us and 21.5, one of 30 001 94 and 71, and no faster for few rows; 256 sequences of 2112 rows,
+// whose blocks are two to a CU then, take 39.5 with them and 54 so)
+constexpr int NT = 1024;
+// of the histogram, a lane's the even or the odd one (30 001 rows whose survivors are in place, selection that is: 30.8 us with one, 29.8 with two, at that time; of
+// 71 us with moves it makes nothing that can be measured; four do not fit beside the weights)
+constexpr int kCopies = 2;
 constexpr int kAtOnce = 4;          // 16-byte pieces of rows that a thread moves in a turn
 
 // Weights in ascending order as whole numbers: 0 is a row that is not in the cache, NaN the greatest, -0 and 0 are equal.
@@ -70,8 +76,8 @@ struct ScaleRow {
     }
 };
 
-// The loops are not unrolled: most of a small call's time is fetching code that it runs once (4352 rows: 12.9 us with the weights in registers
-// and every loop over them unrolled, 11.1 us so).
+// The loops are not unrolled: most of a small call's time is fetching code that it runs once (4352 rows, passes over the same states, where 10.3 us are left
+// now: 12.9 us with the weights in registers and every loop over them unrolled, 11.1 us so).
 template <int DQK, int DV, int BITS>
 __global__ void __launch_bounds__(NT)
 attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint8_t* __restrict__ vc, uint8_t* __restrict__ vs,
@@ -182,8 +188,8 @@ attn_cache_evict_kernel(uint8_t* __restrict__ kc, uint8_t* __restrict__ ks, uint
         const uint32_t least = prefix;                     // what survivors begin with at least; `wanted` of those that begin so survive, the first ones
 
         // ---- holes and movers, in ascending order
-        // (8 keys of a thread in a turn where 4 would take more than one: 30 001 rows 29.2 us with 4, 27.2 with 8, 32 sequences of 4352 rows 14.5 and 14.1, of
-        // 8500 rows 19.0 and 19.4; 1088 rows 8.5 and 9.0)
+        // (8 keys of a thread in a turn where 4 would take more than one.  4 and 8, first passes over states: one sequence of 8000 rows 29.2 us and 28.9, 8 of
+        // 30 001 92.9 and 92.1, one of 120 001 247 and 244, 32 of 1088 13.3 and 14.1, 256 of 2112 54.8 and 58.9; later ones: 30 001 rows 44.1 and 42.3)
         auto list = [&](auto of_thread) __attribute__((always_inline)) {
             constexpr int KT = decltype(of_thread)::value;
             int equal = 0;
